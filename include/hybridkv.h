@@ -411,6 +411,106 @@ int hk_paged_decode_attn_absorbed(const hk_shape *shape, const void *q, int32_t 
                                   void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Paged K/V cache in 16 or 8 bits, with shared K/V heads: rows of new tokens written (and quantised as they are
+ * written), rows read back, and the attention of one query token or of a tree of drafted tokens over it.
+ *
+ * Blocks, table and lengths are those of hk_paged_cache (Sec. 4.1).  What differs:
+ *   n_kv_heads   K/V heads; it divides n_heads, and query head h reads K/V head h / (n_heads / n_kv_heads)
+ *   format       HK_KV_16: the pools hold the shape's dtype (fp16 or bf16).  HK_KV_INT8, HK_KV_E4M3 (the OCP 8-bit float
+ *                with a 3-bit mantissa): the pools hold one byte an element and every (token, K/V head) has a scale of its
+ *                own for K and for V; the element is scale * code.
+ *   K_pool, V_pool    [P_kv, n_kv_heads, block_tokens, dh], elements of the format
+ *   K_scale, V_scale  [P_kv, n_kv_heads, block_tokens] fp32, not negative; NULL for HK_KV_16
+ *   act_pool     [P_act, block_tokens, d] and table entries < 0 (ACT blocks): HK_KV_16 with n_kv_heads == n_heads only.  A
+ *                checkpoint takes as many bytes as an 8-bit K/V row pair, so an 8-bit cache has nothing to win from ACT
+ *                blocks: P_act must be 0 there (HK_ERR_SHAPE).
+ *   total_tokens HOST: the sum of seq_len or any upper bound of it (at most B * max_blocks * block_tokens); it sizes the
+ *                launch and the workspace of the attention, and changes no result but by the order of sums
+ * Table and lengths are device data: entries are held to the pools, lengths to the table's row, negative lengths count
+ * as 0, so inconsistent tables give wrong numbers, not stray accesses.
+ * These calls take every dtype of the shape and every format; hk_shape.attn_splits and gemm_tile as everywhere
+ * (attn_splits > 0: the tokens are cut into about that many equal pieces per request).
+ */
+enum { HK_KV_16 = 0, HK_KV_INT8 = 1, HK_KV_E4M3 = 2 };
+enum { HK_TREE_MAX_NODES = 64 };
+
+typedef struct hk_kv_cache {
+    void *K_pool, *V_pool;
+    float *K_scale, *V_scale;
+    void *act_pool;
+    const int32_t *block_table;    /* [B, max_blocks], device */
+    const int32_t *seq_len;        /* [B], device */
+    int64_t total_tokens;
+    int32_t P_kv, P_act, n_act_used;
+    int32_t block_tokens;          /* a power of two, 16 .. 1024 */
+    int32_t max_blocks;
+    int32_t n_kv_heads;
+    int32_t format;
+} hk_kv_cache;
+
+/*
+ * Writes the K/V rows of new tokens into the cache: a prompt, one token, or the accepted path of a drafted tree.
+ * seq_len counts them already: the n new tokens of request r are its last n, tokens seq_len[r] - n .. seq_len[r] - 1, as
+ * hk_qkv_current_paged has it.
+ *   k, v    [B, T, n_kv_heads, dh], the shape's dtype: what hk_qkv_current leaves in K_dst, V_dst [B * T, n_heads, 1, dh]
+ *   x       [B, T, d] layer inputs, or NULL: new tokens whose block is an ACT block get this row there (without x: nothing)
+ *   n_new   [B] int32, device, or NULL (= T everywhere): new tokens of the request, taken as 0 .. T
+ *   pick    [B, T] int32, device, or NULL: the row (0 .. T - 1) of k, v, x that holds the request's i-th new token; NULL: row
+ *           i.  The same row may be picked twice; a token whose pick lies outside is not written.
+ * A row is quantised from its dh elements:
+ *     scale = max(max |x| / Q, 2^-100),  code = x / scale rounded to nearest even     (fp32; Q = 127 int8, 448 e4m3)
+ * so that an element is off by at most half a step of the format at its scale.  A row that holds an infinity or a NaN
+ * gets the scale NaN and reads back as NaN.  HK_KV_16 rows are copied.
+ * Only the rows of new tokens are written; tokens before 0 or behind the table's row, and entries outside the pools, are
+ * not.  Requests that share a block must not write the same token in one call.  k and v may be NULL together when P_kv == 0.
+ */
+int hk_kv_store(const hk_shape *shape, const void *k, const void *v, const void *x, int32_t B, int32_t T,
+                const int32_t *n_new, const int32_t *pick, const hk_kv_cache *cache, void *stream);
+
+/*
+ * Reads rows back: token tok_off + i of request r to row i of K_out[r], V_out[r], for i < L_cap and tok_off + i < seq_len[r],
+ * as scale * code rounded once to the shape's dtype.
+ *   K_out, V_out  [B, n_kv_heads, L_cap, dh], the shape's dtype: the layout of K_cache, V_cache of hk_hybrid_decode_attn
+ * Other rows, and rows of tokens that sit in ACT blocks, are left as they are.
+ */
+int hk_kv_load(const hk_shape *shape, void *K_out, void *V_out, int32_t B, int32_t tok_off, int32_t L_cap,
+               const hk_kv_cache *cache, void *stream);
+
+/*
+ * Attention of one query token a request over its seq_len tokens (Eq. 4), as hk_paged_decode_attn, for every format and
+ * for shared K/V heads.  ACT blocks are regenerated into the workspace first (params as for hk_paged_decode_attn; NULL when
+ * n_act_used == 0).  A request without tokens gets an all-zero output.
+ *   q, out     [B, n_heads, dh]
+ *   workspace  hk_kv_attn_workspace_bytes(shape, B, 1, cache); scratch only, nothing in it needs clearing
+ * The probabilities are held in fp32; for the product with V they are rounded to the shape's dtype (HK_KV_16), or, taken
+ * times the scales of V and relative to their running maximum, to fp16 (8-bit formats).
+ */
+size_t hk_kv_attn_workspace_bytes(const hk_shape *shape, int32_t B, int32_t T, const hk_kv_cache *cache);
+int hk_kv_decode_attn(const hk_shape *shape, const void *q, int32_t B, const hk_kv_cache *cache,
+                      const hk_layer_params *params, void *out,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention for a tree of drafted tokens over the cache: node i of request r attends to all seq_len[r] tokens of the
+ * cache and to those nodes of its own request that its mask names.
+ *   q, out     [B, T, n_heads, dh], 1 <= T <= HK_TREE_MAX_NODES
+ *   k, v       [B, T, n_kv_heads, dh], the shape's dtype: the nodes' own rows, which are not in the cache (hk_kv_store
+ *              writes the accepted ones afterwards); seq_len does not count them
+ *   mask       int64, device, or NULL: bit j of mask[r * mask_stride + i] says that node i sees node j (a tree: its
+ *              ancestors and itself); any pattern is allowed.  mask_stride T: a mask per request, 0: one for all.  NULL:
+ *              a chain, node i sees nodes 0 .. i.  Bits of nodes that the request does not have are ignored.
+ *   n_nodes    [B] int32, device, or NULL (= T everywhere): nodes of the request, taken as 0 .. T; the output rows of
+ *              the other nodes are left as they are
+ * A node that sees nothing (no cached token, an empty mask) gets an all-zero output.  What a node does not see, infinities
+ * and NaN included, has no influence on its output.
+ *   workspace  hk_kv_attn_workspace_bytes(shape, B, T, cache); otherwise as hk_kv_decode_attn
+ */
+int hk_kv_tree_attn(const hk_shape *shape, const void *q, const void *k, const void *v, int32_t B, int32_t T,
+                    const int64_t *mask, int32_t mask_stride, const int32_t *n_nodes, const hk_kv_cache *cache,
+                    const hk_layer_params *params, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Cache-management policy arithmetic (Sec. 4.3).  Host-only: every pointer below is a HOST pointer,
  * nothing touches a device.  Times are in any one unit, sizes in any one unit; block counts are real
  * numbers inside the models and whole blocks (rounded down) in the results.

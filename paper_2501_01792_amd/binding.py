@@ -51,6 +51,18 @@ class hk_paged_cache(ctypes.Structure):
                 ("n_act_used", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("max_blocks", ctypes.c_int32)]
 
 
+HK_KV_16, HK_KV_INT8, HK_KV_E4M3 = 0, 1, 2
+HK_TREE_MAX_NODES = 64
+
+
+class hk_kv_cache(ctypes.Structure):
+    _fields_ = [("K_pool", ctypes.c_void_p), ("V_pool", ctypes.c_void_p), ("K_scale", ctypes.c_void_p),
+                ("V_scale", ctypes.c_void_p), ("act_pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p), ("total_tokens", ctypes.c_int64), ("P_kv", ctypes.c_int32),
+                ("P_act", ctypes.c_int32), ("n_act_used", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
 class hk_layer_params(ctypes.Structure):
     _fields_ = [("ln_w", ctypes.c_void_p), ("ln_b", ctypes.c_void_p),
                 ("Wkv", ctypes.c_void_p), ("bkv", ctypes.c_void_p), ("prepared", ctypes.c_void_p)]
@@ -120,6 +132,17 @@ def lib():
         L.hk_qkv_current_paged.restype = ctypes.c_int
         L.hk_qkv_current_paged.argtypes = [ctypes.POINTER(hk_shape), vp, i32, ctypes.POINTER(hk_layer_params), vp, vp, vp,
                                            ctypes.POINTER(hk_paged_cache), vp, vp, sz, vp]
+        kvp = ctypes.POINTER(hk_kv_cache)
+        L.hk_kv_store.restype = ctypes.c_int
+        L.hk_kv_store.argtypes = [shp, vp, vp, vp, i32, i32, vp, vp, kvp, vp]
+        L.hk_kv_load.restype = ctypes.c_int
+        L.hk_kv_load.argtypes = [shp, vp, vp, i32, i32, i32, kvp, vp]
+        L.hk_kv_attn_workspace_bytes.restype = sz
+        L.hk_kv_attn_workspace_bytes.argtypes = [shp, i32, i32, kvp]
+        L.hk_kv_decode_attn.restype = ctypes.c_int
+        L.hk_kv_decode_attn.argtypes = [shp, vp, i32, kvp, lpp, vp, vp, sz, vp]
+        L.hk_kv_tree_attn.restype = ctypes.c_int
+        L.hk_kv_tree_attn.argtypes = [shp, vp, vp, vp, i32, i32, vp, i32, vp, kvp, lpp, vp, vp, sz, vp]
         dp = ctypes.POINTER(ctypes.c_double)
         L.hk_fit_line.restype = ctypes.c_int
         L.hk_fit_line.argtypes = [dp, dp, i32, ctypes.POINTER(hk_line), dp]
@@ -560,3 +583,230 @@ def paged_decode_attn(q, K_pool, V_pool, act_pool, block_table, seq_len, block_t
     if st != HK_OK:
         raise HybridKVError(st, "hk_paged_decode_attn_absorbed" if absorbed else "hk_paged_decode_attn")
     return out
+
+
+# ----------------------------------------------------------------------------- paged K/V cache in 16 or 8 bits
+class KvCache:
+    """Handle of a paged K/V cache (hk_kv_cache): its tensors, kept alive, and the C struct that names them.  Made once by
+    ``make_kv_cache``; the tensors are used where they are, so a change of their contents is seen by the next call."""
+
+    __slots__ = ("struct", "ref", "tensors", "device", "pool_dtype", "B", "n_kv_heads", "head_dim", "d_act", "shapes")
+
+
+def make_kv_cache(K_pool, V_pool, block_table, seq_len, block_tokens, K_scale=None, V_scale=None, act_pool=None, n_act_used=None,
+                  total_tokens=None) -> KvCache:
+    """Handle for ``kv_store``, ``kv_load``, ``kv_decode_attn`` and ``kv_tree_attn``: ``K_pool, V_pool[P_kv, n_kv_heads,
+    block_tokens, dh]`` in fp16 or bf16, or in int8 or float8_e4m3fn with ``K_scale, V_scale[P_kv, n_kv_heads, block_tokens]``
+    fp32; ``block_table[B, max_blocks]`` and ``seq_len[B]`` int32; ``act_pool[P_act, block_tokens, d]`` of a 16-bit cache with
+    ACT blocks.  ``total_tokens``: the sum of ``seq_len`` or an upper bound (default: all that the table has room for)."""
+    import torch
+    formats = {torch.float16: HK_KV_16, torch.bfloat16: HK_KV_16, torch.int8: HK_KV_INT8, torch.float8_e4m3fn: HK_KV_E4M3}
+    if K_pool.dtype not in formats:
+        raise TypeError("K_pool must be float16, bfloat16, int8 or float8_e4m3fn")
+    if K_pool.dim() != 4 or V_pool.shape != K_pool.shape or K_pool.shape[2] != block_tokens:
+        raise ValueError("K_pool, V_pool: [P_kv, n_kv_heads, block_tokens, dh]")
+    if block_table.dim() != 2 or seq_len.shape != block_table.shape[:1]:
+        raise ValueError("block_table: [B, max_blocks], seq_len: [B]")
+    form = formats[K_pool.dtype]
+    if (form != HK_KV_16) != (K_scale is not None) or (K_scale is None) != (V_scale is None):
+        raise ValueError("K_scale and V_scale belong to int8 and float8_e4m3fn pools")
+    if K_scale is not None and (K_scale.shape != K_pool.shape[:3] or V_scale.shape != K_pool.shape[:3]):
+        raise ValueError("K_scale, V_scale: [P_kv, n_kv_heads, block_tokens]")
+    if act_pool is not None and (act_pool.dim() != 3 or act_pool.shape[1] != block_tokens):
+        raise ValueError("act_pool: [P_act, block_tokens, d]")
+    ptr, el = _dev_ptr, K_pool.dtype
+    c = KvCache()
+    c.tensors = (K_pool, V_pool, K_scale, V_scale, act_pool, block_table, seq_len)
+    c.device = K_pool.device
+    _one_device(c.device, *c.tensors)
+    c.pool_dtype, c.B, (_, c.n_kv_heads, _, c.head_dim) = el, block_table.shape[0], K_pool.shape
+    c.d_act = None if act_pool is None else act_pool.shape[2]
+    P_act = 0 if act_pool is None else act_pool.shape[0]
+    room = c.B * block_table.shape[1] * block_tokens
+    c.struct = hk_kv_cache(ptr(K_pool, "K_pool", el), ptr(V_pool, "V_pool", el), ptr(K_scale, "K_scale", torch.float32),
+                           ptr(V_scale, "V_scale", torch.float32), ptr(act_pool, "act_pool", el),
+                           ptr(block_table, "block_table", torch.int32), ptr(seq_len, "seq_len", torch.int32),
+                           room if total_tokens is None else int(total_tokens), K_pool.shape[0], P_act,
+                           P_act if n_act_used is None else int(n_act_used), int(block_tokens), block_table.shape[1],
+                           c.n_kv_heads, form)
+    c.ref = ctypes.byref(c.struct)
+    c.shapes = {}
+    return c
+
+
+def _one_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("tensors on different devices: %s and %s" % (device, t.device))
+
+
+def _kv_shape(cache, n_heads, el, scale=0.0, splits=0, ln_eps=1e-5):
+    """The hk_shape of a call, made once per kind of call and kept with the cache's handle."""
+    key = (n_heads, el, scale, splits, ln_eps)
+    ref = cache.shapes.get(key)
+    if ref is None:
+        import torch
+        if el not in (torch.float16, torch.bfloat16) or cache.struct.format == HK_KV_16 and el != cache.pool_dtype:
+            raise TypeError("rows and queries are float16 or bfloat16, and of the pools' type where these hold 16 bits")
+        shape = hk_shape(n_heads * cache.head_dim, n_heads, cache.head_dim,
+                         HK_DTYPE_BF16 if el == torch.bfloat16 else HK_DTYPE_F16, ln_eps, scale, splits, 0)
+        ref = cache.shapes[key] = ctypes.byref(shape)
+    return ref
+
+
+class _on:
+    """The device of the tensors as the current one for a call, and the stream's handle: ``stream``, or the device's current
+    stream.  What the call allocates inside belongs to that stream."""
+
+    __slots__ = ("device", "stream", "guards")
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.guards = device, stream, ()
+
+    def __enter__(self):
+        import torch
+        if self.stream is not None:
+            if self.stream.device != self.device:
+                raise ValueError("the stream is on %s, the tensors are on %s" % (self.stream.device, self.device))
+            guard = torch.cuda.stream(self.stream)             # sets the device, too
+            guard.__enter__()
+            self.guards = (guard,)
+            return self.stream.cuda_stream
+        if torch.cuda.current_device() != self.device.index:
+            guard = torch.cuda.device(self.device)
+            guard.__enter__()
+            self.guards = (guard,)
+        return _stream_ptr(None)
+
+    def __exit__(self, *exc):
+        for guard in self.guards:
+            guard.__exit__(*exc)
+        return False
+
+
+def kv_store(cache, k, v, x=None, n_new=None, pick=None, stream=None):
+    """hk_kv_store: the rows ``k, v[B, T, n_kv_heads, dh]`` of new tokens into the cache, the last ``n_new[b]`` (int32; default
+    T) of the ``seq_len[b]`` tokens of each request, quantised where the pools hold 8 bits.  ``pick[B, T]`` int32: the row of
+    each new token (the accepted path of a tree).  ``x[B, T, d]``: layer inputs, stored where the block is an ACT block."""
+    import torch
+    B, T = k.shape[:2]
+    if k.shape != v.shape or k.dim() != 4 or B != cache.B or k.shape[2:] != (cache.n_kv_heads, cache.head_dim):
+        raise ValueError("k, v: [B, T, n_kv_heads, dh] of the cache")
+    if x is not None and x.shape != (B, T, cache.n_kv_heads * cache.head_dim):
+        raise ValueError("x: [B, T, d]")
+    if n_new is not None and n_new.shape != (B,) or pick is not None and pick.shape != (B, T):
+        raise ValueError("n_new: [B], pick: [B, T]")
+    el = k.dtype
+    shape = _kv_shape(cache, cache.n_kv_heads, el)
+    _one_device(cache.device, k, v, x, n_new, pick)
+    args = (_dev_ptr(k, "k", el), _dev_ptr(v, "v", el), _dev_ptr(x, "x", el), B, T, _dev_ptr(n_new, "n_new", torch.int32),
+            _dev_ptr(pick, "pick", torch.int32))
+    with _on(cache.device, stream) as handle:
+        st = lib().hk_kv_store(shape, *args, cache.ref, handle)
+    if st != HK_OK:
+        raise HybridKVError(st, "hk_kv_store")
+
+
+def kv_load(cache, L_cap, tok_off=0, dtype=None, K_out=None, V_out=None, stream=None):
+    """hk_kv_load: tokens ``tok_off .. tok_off + L_cap - 1`` of every request as ``K, V[B, n_kv_heads, L_cap, dh]`` in ``dtype``
+    (default: that of ``K_out``, of 16-bit pools, or float16).  Rows without a cached token are left as they are, zeros where
+    the outputs are allocated here."""
+    import torch
+    if dtype is None:
+        dtype = K_out.dtype if K_out is not None else cache.pool_dtype if cache.struct.format == HK_KV_16 else torch.float16
+    size = (cache.B, cache.n_kv_heads, L_cap, cache.head_dim)
+    if (K_out is None) != (V_out is None) or K_out is not None and (tuple(K_out.shape) != size or tuple(V_out.shape) != size):
+        raise ValueError("K_out, V_out: [B, n_kv_heads, L_cap, dh]")
+    shape = _kv_shape(cache, cache.n_kv_heads, dtype)
+    _one_device(cache.device, K_out, V_out)
+    with _on(cache.device, stream) as handle:
+        if K_out is None:
+            K_out, V_out = (torch.zeros(size, dtype=dtype, device=cache.device) for _ in range(2))
+        st = lib().hk_kv_load(shape, _dev_ptr(K_out, "K_out", dtype), _dev_ptr(V_out, "V_out", dtype), cache.B, tok_off, L_cap,
+                              cache.ref, handle)
+    if st != HK_OK:
+        raise HybridKVError(st, "hk_kv_load")
+    return K_out, V_out
+
+
+def kv_attn_workspace_bytes(q, cache, attn_splits=0) -> int:
+    """hk_kv_attn_workspace_bytes for ``kv_decode_attn`` (``q[B, H, dh]``) or ``kv_tree_attn`` (``q[B, T, H, dh]``)."""
+    T, H = (1, q.shape[1]) if q.dim() == 3 else q.shape[1:3]
+    return int(lib().hk_kv_attn_workspace_bytes(_kv_shape(cache, H, q.dtype, 0.0, attn_splits), cache.B, T, cache.ref))
+
+
+def _kv_attend(entry, where, q, rows, tail, cache, T, H, layer_params, out, workspace, softmax_scale, attn_splits, stream,
+               ln_eps):
+    import torch
+    el = q.dtype
+    if q.shape[0] != cache.B or q.shape[-1] != cache.head_dim:
+        raise ValueError("q: [B, H, dh] or [B, T, H, dh] of the cache's B and dh")
+    if out is not None and out.shape != q.shape:
+        raise ValueError("out: the shape of q")
+    shape = _kv_shape(cache, H, el, softmax_scale, attn_splits, ln_eps)
+    lp = None
+    if layer_params is not None:
+        if cache.d_act is not None and cache.d_act != H * cache.head_dim or layer_params[0].shape[0] != H * cache.head_dim:
+            raise ValueError("act_pool and the layer: d = H * dh")
+        lp = ctypes.byref(_params(*layer_params, el=el))
+        _one_device(cache.device, *layer_params)
+    elif cache.struct.n_act_used > 0:
+        raise ValueError("a cache with ACT blocks in use needs layer_params")
+    _one_device(cache.device, q, out, workspace)
+    with _on(cache.device, stream) as handle:
+        if out is None:
+            out = torch.empty_like(q) if T is None else torch.zeros_like(q)
+        if workspace is None:
+            workspace = new_workspace(kv_attn_workspace_bytes(q, cache, attn_splits), cache.device)
+        st = entry(shape, _dev_ptr(q, "q", el), *rows, cache.B, *tail, cache.ref, lp, _dev_ptr(out, "out", el),
+                   _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), handle)
+    if st != HK_OK:
+        raise HybridKVError(st, where)
+    return out
+
+
+def kv_decode_attn(q, cache, layer_params=None, out=None, workspace=None, softmax_scale=0.0, attn_splits=0, stream=None,
+                   ln_eps=1e-5):
+    """hk_kv_decode_attn: the query ``q[B, H, dh]`` of one token a request over the ``seq_len[b]`` tokens of the cache ->
+    ``out[B, H, dh]``.  H is a multiple of the cache's n_kv_heads.  ``layer_params`` as everywhere, for ACT blocks."""
+    if q.dim() != 3:
+        raise ValueError("q: [B, H, dh]")
+    return _kv_attend(lib().hk_kv_decode_attn, "hk_kv_decode_attn", q, (), (), cache, None, q.shape[1], layer_params, out, workspace,
+                      softmax_scale, attn_splits, stream, ln_eps)
+
+
+def kv_tree_attn(q, k, v, cache, mask=None, n_nodes=None, layer_params=None, out=None, workspace=None, softmax_scale=0.0,
+                 attn_splits=0, stream=None, ln_eps=1e-5):
+    """hk_kv_tree_attn: ``q[B, T, H, dh]`` and the rows ``k, v[B, T, n_kv_heads, dh]`` of T <= 64 drafted tokens a request ->
+    ``out[B, T, H, dh]``: node i attends to the request's cached tokens and to the nodes j whose bit is set in ``mask[B, T]`` or
+    ``mask[T]`` (int64, ``tree_mask``; default: a chain).  ``n_nodes[B]`` int32: nodes of each request; the output rows of the
+    others are left as they are, zeros where ``out`` is allocated here."""
+    import torch
+    if q.dim() != 4:
+        raise ValueError("q: [B, T, H, dh]")
+    B, T, H, dh = q.shape
+    size = (B, T, cache.n_kv_heads, cache.head_dim)
+    if tuple(k.shape) != size or tuple(v.shape) != size:
+        raise ValueError("k, v: [B, T, n_kv_heads, dh]")
+    if mask is not None and tuple(mask.shape) not in ((B, T), (T,)) or n_nodes is not None and tuple(n_nodes.shape) != (B,):
+        raise ValueError("mask: [B, T] or [T], n_nodes: [B]")
+    _one_device(cache.device, k, v, mask, n_nodes)
+    rows = (_dev_ptr(k, "k", q.dtype), _dev_ptr(v, "v", q.dtype))
+    tail = (T, _dev_ptr(mask, "mask", torch.int64), T if mask is not None and mask.dim() == 2 else 0,
+            _dev_ptr(n_nodes, "n_nodes", torch.int32))
+    return _kv_attend(lib().hk_kv_tree_attn, "hk_kv_tree_attn", q, rows, tail, cache, T, H, layer_params, out, workspace, softmax_scale,
+                      attn_splits, stream, ln_eps)
+
+
+def tree_mask(parents):
+    """The mask of a tree for ``kv_tree_attn``: ``parents[i]`` is the node that node i follows, an earlier one, or -1 where it
+    follows the context.  Returns int64 on the host, bit j of entry i: node i sees node j (its ancestors and itself)."""
+    import torch
+    if len(parents) > HK_TREE_MAX_NODES:
+        raise ValueError("a tree has at most %d nodes" % HK_TREE_MAX_NODES)
+    bits = []
+    for i, parent in enumerate(parents):
+        if not -1 <= parent < i:
+            raise ValueError("node %d follows node %d: a parent comes earlier (or is -1)" % (i, parent))
+        bits.append((bits[parent] if parent >= 0 else 0) | 1 << i)
+    return torch.tensor([b - (1 << 64) if b >> 63 else b for b in bits], dtype=torch.int64)

@@ -19,7 +19,8 @@ PROBE_SRC = [os.path.join(HERE, "probe", "mfma_rate.hip"),     # measurement aid
 PROBE_LIB = os.path.join(HERE, "probe", "libhkprobe.so")
 PROBE_LT_SRC = os.path.join(HERE, "probe", "library_gemm.hip")  # the vendor GEMM's candidate kernels, timed (links hipBLASLt)
 PROBE_LT_LIB = os.path.join(HERE, "probe", "libhkprobe_lt.so")
-SOURCES = ["api.hip", "device_info.hip", "ln_stats.hip", "kv_gemm.hip", "kv_gemm_fold.hip", "kv_gemm_tile.hip", "flash_decode.hip", "paged_decode.hip", "paged_append.hip", "qkv_current.hip", "qkv_stream.hip", "absorbed.hip", "absorbed_stream.hip", "policy.hip"]
+SOURCES = ["api.hip", "device_info.hip", "ln_stats.hip", "kv_gemm.hip", "kv_gemm_fold.hip", "kv_gemm_tile.hip", "flash_decode.hip", "paged_decode.hip", "paged_append.hip", "qkv_current.hip", "qkv_stream.hip", "absorbed.hip", "absorbed_stream.hip", "policy.hip",
+           "kv_cache.hip", "kv_attn.hip", "kv_attn_16.hip", "kv_attn_int8.hip", "kv_attn_e4m3.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -44,7 +45,7 @@ def build(verbose: bool = False) -> str:
             print(r.stderr, file=sys.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(compile_one, SOURCES))
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp])

@@ -1001,3 +1001,188 @@ int hk_paged_append(int32_t *block_table, int32_t *seq_len, int64_t *cu_tokens, 
     if (hk::launch_paged_append(a, static_cast<hipStream_t>(stream)) != hipSuccess) return HK_ERR_LAUNCH;
     return HK_OK;
 }
+
+// --------------------------------------------------------------- paged K/V cache in 16 or 8 bits, shared K/V heads
+namespace {
+
+// Checks of the sizes that every call makes; fills the kernels' view.
+int kv_view(const hk_shape *s, int64_t B, const hk_kv_cache *c, hk::KvCacheView *v)
+{
+    const int st = check_shape(s);
+    if (st != HK_OK) return st;
+    if (!c) return HK_ERR_NULL;
+    if (c->format != HK_KV_16 && c->format != HK_KV_INT8 && c->format != HK_KV_E4M3) return HK_ERR_DTYPE;
+    if (B < 0 || B > (1 << 20)) return HK_ERR_SHAPE;
+    if (c->n_kv_heads <= 0 || s->n_heads % c->n_kv_heads != 0) return HK_ERR_SHAPE;
+    const int bt = c->block_tokens;
+    if (bt < 16 || bt > 1024 || (bt & (bt - 1)) != 0) return HK_ERR_SHAPE;
+    if (c->P_kv < 0 || c->P_act < 0 || c->n_act_used < 0 || c->n_act_used > c->P_act || c->max_blocks < 0) return HK_ERR_SHAPE;
+    if ((int64_t)c->max_blocks * bt > (1 << 30) || B * c->max_blocks > 0x7fffffffLL) return HK_ERR_SHAPE;
+    if (c->total_tokens < 0 || c->total_tokens > B * c->max_blocks * bt) return HK_ERR_SHAPE;
+    // checkpoints: a 16-bit cache of a layer whose query heads have K/V heads of their own
+    if (c->P_act > 0 && (c->format != HK_KV_16 || c->n_kv_heads != s->n_heads)) return HK_ERR_SHAPE;
+    const long double elems = ((long double)c->P_kv * c->n_kv_heads * s->head_dim + (long double)c->P_act * s->d) * bt;
+    if (elems > 4.0e12L) return HK_ERR_SHAPE;
+    int blk_log2 = 0;
+    while ((1 << blk_log2) < bt) ++blk_log2;
+    v->K_pool = c->K_pool; v->V_pool = c->V_pool; v->K_scale = c->K_scale; v->V_scale = c->V_scale;
+    v->block_table = c->block_table; v->seq_len = c->seq_len;
+    v->max_blocks = c->max_blocks; v->blk_log2 = blk_log2; v->P_kv = c->P_kv; v->P_act = c->P_act; v->Hkv = c->n_kv_heads;
+    return HK_OK;
+}
+
+// The cache's pointers, for calls that have work to do.
+int kv_pointers(const hk_kv_cache *c)
+{
+    if (!c->block_table || !c->seq_len) return HK_ERR_NULL;
+    if (!aligned(c->block_table, 4) || !aligned(c->seq_len, 4)) return HK_ERR_ALIGN;
+    if (c->P_kv > 0) {
+        if (!c->K_pool || !c->V_pool) return HK_ERR_NULL;
+        if (c->format != HK_KV_16 && (!c->K_scale || !c->V_scale)) return HK_ERR_NULL;
+        if (!aligned(c->K_pool, 16) || !aligned(c->V_pool, 16) || !aligned(c->K_scale, 16) || !aligned(c->V_scale, 16)) return HK_ERR_ALIGN;
+    }
+    if (c->P_act > 0) {
+        if (!c->act_pool) return HK_ERR_NULL;
+        if (!aligned(c->act_pool, 16)) return HK_ERR_ALIGN;
+    }
+    return HK_OK;
+}
+
+struct KvAttnPlan {
+    hk::KvCacheView view;
+    int64_t M;                 // rows of the regeneration
+    float scale;
+    size_t off_k, off_v, off_stats, off_prep, off_partial, total;
+};
+
+int make_kv_attn_plan(const hk_shape *s, int64_t B, int64_t T, const hk_kv_cache *c, KvAttnPlan *p)
+{
+    const int st = kv_view(s, B, c, &p->view);
+    if (st != HK_OK) return st;
+    if (T < 1 || T > HK_TREE_MAX_NODES) return HK_ERR_SHAPE;
+    if (c->total_tokens > 0 && c->P_kv == 0 && c->n_act_used == 0) return HK_ERR_SHAPE;      // tokens but no block to hold them
+    p->view.P_act = c->n_act_used;
+    if (c->P_kv == 0 && c->n_act_used == 0) p->view.max_blocks = 0;                          // whatever the lengths say
+    if (!hk::kv_attn_launchable(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, c->total_tokens, s->attn_splits)) return HK_ERR_SHAPE;
+    p->M = (int64_t)c->n_act_used * c->block_tokens;
+    if (p->M > 0x7fffffffLL) return HK_ERR_SHAPE;
+    p->scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / std::sqrt((float)s->head_dim);
+    const size_t kv_bytes = align_up((size_t)p->M * s->d * 2);
+    p->off_k = 0;
+    p->off_v = kv_bytes;
+    p->off_stats = 2 * kv_bytes;
+    p->off_prep = p->off_stats + align_up((size_t)p->M * sizeof(float2));
+    p->off_partial = p->off_prep;
+    if (p->M > 0 && hk::kv_gemm_uses_prepared(p->M, s->d, s->gemm_tile, s->dtype)) p->off_partial += prepared_layout(s->d).total;
+    const size_t floats = hk::kv_attn_partial_floats(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, c->total_tokens, s->attn_splits);
+    p->total = p->off_partial + align_up(floats * sizeof(float));
+    return HK_OK;
+}
+
+int kv_attn_impl(const hk_shape *shape, const void *q, const void *k, const void *v, int32_t B, int32_t T, const int64_t *mask,
+                 int32_t mask_stride, const int32_t *n_nodes, const hk_kv_cache *cache, const hk_layer_params *params, void *out,
+                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    KvAttnPlan p;
+    int st = make_kv_attn_plan(shape, B, T, cache, &p);
+    if (st != HK_OK) return st;
+    if (B == 0) return HK_OK;
+    if (!q || !out || !workspace) return HK_ERR_NULL;
+    st = kv_pointers(cache);
+    if (st != HK_OK) return st;
+    if (cache->n_act_used > 0) {
+        st = check_params(params);
+        if (st != HK_OK) return st;
+    }
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(workspace, kAlign)) return HK_ERR_ALIGN;
+    if (!aligned(mask, 8) || !aligned(n_nodes, 4)) return HK_ERR_ALIGN;
+    if (workspace_bytes < p.total) return HK_ERR_WORKSPACE;
+
+    char *ws = static_cast<char *>(workspace);
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    hk::KvAttnArgs a;
+    a.K_regen = nullptr; a.V_regen = nullptr;
+    if (cache->n_act_used > 0) {
+        // as in hk_paged_decode_attn: the rows of ACT block b land in block b of pools of the KV pool's layout
+        st = regen_impl(shape, cache->act_pool, cache->block_tokens, params, ws + p.off_k, ws + p.off_v, cache->block_tokens, 0,
+                        reinterpret_cast<float2 *>(ws + p.off_stats), ws + p.off_prep, p.M, hs, Marks{nullptr, 0, nullptr});
+        if (st != HK_OK) return st;
+        a.K_regen = ws + p.off_k; a.V_regen = ws + p.off_v;
+    }
+    a.c = p.view;
+    a.q = q; a.k = k; a.v = v; a.mask = mask; a.n_nodes = n_nodes; a.out = out;
+    a.partial = reinterpret_cast<float *>(ws + p.off_partial);
+    a.B = B; a.T = T; a.H = shape->n_heads; a.mask_stride = mask_stride; a.head_dim = shape->head_dim;
+    a.format = cache->format; a.dtype = shape->dtype; a.total_tokens = cache->total_tokens; a.splits = shape->attn_splits;
+    a.scale = p.scale;
+    if (hk::launch_kv_attn(a, hs) != hipSuccess) return HK_ERR_LAUNCH;
+    return HK_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hk_kv_store(const hk_shape *shape, const void *k, const void *v, const void *x, int32_t B, int32_t T,
+                const int32_t *n_new, const int32_t *pick, const hk_kv_cache *cache, void *stream)
+{
+    hk::KvStoreArgs a;
+    int st = kv_view(shape, B, cache, &a.c);
+    if (st != HK_OK) return st;
+    if (T < 0 || (int64_t)B * ((int64_t)T + 15) * cache->n_kv_heads > (1 << 27)) return HK_ERR_SHAPE;
+    if (!k != !v) return HK_ERR_NULL;
+    if (B == 0 || T == 0) return HK_OK;
+    st = kv_pointers(cache);
+    if (st != HK_OK) return st;
+    if (cache->P_kv > 0 && !k) return HK_ERR_NULL;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(x, 16) || !aligned(n_new, 4) || !aligned(pick, 4)) return HK_ERR_ALIGN;
+    a.k = k; a.v = v; a.x = x; a.act_pool = cache->act_pool; a.n_new = n_new; a.pick = pick;
+    a.B = B; a.T = T; a.head_dim = shape->head_dim; a.d = shape->d; a.format = cache->format; a.dtype = shape->dtype;
+    if (hk::launch_kv_store(a, static_cast<hipStream_t>(stream)) != hipSuccess) return HK_ERR_LAUNCH;
+    return HK_OK;
+}
+
+int hk_kv_load(const hk_shape *shape, void *K_out, void *V_out, int32_t B, int32_t tok_off, int32_t L_cap,
+               const hk_kv_cache *cache, void *stream)
+{
+    hk::KvLoadArgs a;
+    int st = kv_view(shape, B, cache, &a.c);
+    if (st != HK_OK) return st;
+    if (tok_off < 0 || L_cap < 0 || tok_off > (1 << 30) || L_cap > (1 << 30)) return HK_ERR_SHAPE;
+    if ((int64_t)B * cache->n_kv_heads * (((int64_t)L_cap + 63) / 64) > (1 << 23)) return HK_ERR_SHAPE;
+    if (B == 0 || L_cap == 0) return HK_OK;
+    st = kv_pointers(cache);
+    if (st != HK_OK) return st;
+    if (!K_out || !V_out) return HK_ERR_NULL;
+    if (!aligned(K_out, 16) || !aligned(V_out, 16)) return HK_ERR_ALIGN;
+    a.K_out = K_out; a.V_out = V_out; a.B = B; a.tok_off = tok_off; a.L_cap = L_cap; a.head_dim = shape->head_dim;
+    a.format = cache->format; a.dtype = shape->dtype;
+    if (hk::launch_kv_load(a, static_cast<hipStream_t>(stream)) != hipSuccess) return HK_ERR_LAUNCH;
+    return HK_OK;
+}
+
+size_t hk_kv_attn_workspace_bytes(const hk_shape *shape, int32_t B, int32_t T, const hk_kv_cache *cache)
+{
+    KvAttnPlan p;
+    if (make_kv_attn_plan(shape, B, T, cache, &p) != HK_OK) return 0;
+    return p.total > 0 ? p.total : kAlign;
+}
+
+int hk_kv_decode_attn(const hk_shape *shape, const void *q, int32_t B, const hk_kv_cache *cache,
+                      const hk_layer_params *params, void *out,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    return kv_attn_impl(shape, q, nullptr, nullptr, B, 1, nullptr, 0, nullptr, cache, params, out, workspace, workspace_bytes, stream);
+}
+
+int hk_kv_tree_attn(const hk_shape *shape, const void *q, const void *k, const void *v, int32_t B, int32_t T,
+                    const int64_t *mask, int32_t mask_stride, const int32_t *n_nodes, const hk_kv_cache *cache,
+                    const hk_layer_params *params, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (mask && mask_stride != 0 && mask_stride != T) return HK_ERR_SHAPE;
+    if (B > 0 && (!k || !v)) return HK_ERR_NULL;
+    return kv_attn_impl(shape, q, k, v, B, T, mask, mask_stride, n_nodes, cache, params, out, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

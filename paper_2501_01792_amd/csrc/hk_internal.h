@@ -219,4 +219,50 @@ hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t s);
 hipError_t launch_paged_index(const PagedAbsorbedArgs &a, hipStream_t s);
 hipError_t launch_paged_absorbed(const PagedAbsorbedArgs &a, hipStream_t s);
 
+// The paged K/V cache in 16 or 8 bits as the kernels see it; format as in the C ABI (0: 16 bits, 1: int8, 2: e4m3).
+struct KvCacheView {
+    void *K_pool, *V_pool;             // [P_kv, Hkv, 2^blk_log2, dh]
+    float *K_scale, *V_scale;          // [P_kv, Hkv, 2^blk_log2], 8-bit formats
+    const int32_t *block_table;        // [B, max_blocks]: >= 0 KV block number, < 0 ACT block ~entry
+    const int32_t *seq_len;            // [B]
+    int max_blocks, blk_log2, P_kv, P_act, Hkv;
+};
+struct KvStoreArgs {
+    KvCacheView c;
+    const void *k, *v;                 // [B, T, Hkv, dh]
+    const void *x;                     // optional [B, T, d], rows for act_pool
+    void *act_pool;                    // [P_act, 2^blk_log2, d]
+    const int32_t *n_new, *pick;       // optional [B], [B, T]
+    int B, T, head_dim, d, format, dtype;
+};
+// Rows of new tokens into the cache (see kv_cache.hip).
+hipError_t launch_kv_store(const KvStoreArgs &a, hipStream_t s);
+struct KvLoadArgs {
+    KvCacheView c;
+    void *K_out, *V_out;               // [B, Hkv, L_cap, dh]
+    int B, tok_off, L_cap, head_dim, format, dtype;
+};
+// Rows of the cache in 16 bits.
+hipError_t launch_kv_load(const KvLoadArgs &a, hipStream_t s);
+
+struct KvAttnArgs {
+    KvCacheView c;                     // P_act: regenerated blocks
+    const void *K_regen, *V_regen;     // [P_act, Hkv, 2^blk_log2, dh]: regenerated ACT blocks (16-bit format; null when P_act == 0)
+    const void *q;                     // [B, T, H, dh]
+    const void *k, *v;                 // [B, T, Hkv, dh]: the nodes' own rows, or null: queries over the cache alone
+    const int64_t *mask;               // optional: node i of request r sees the nodes of mask[r * mask_stride + i]
+    const int32_t *n_nodes;            // optional [B]
+    void *out;                         // [B, T, H, dh]
+    float *partial;                    // scratch of kv_attn_partial_floats() floats
+    int B, T, H, mask_stride, head_dim, format, dtype;
+    int64_t total_tokens;
+    int splits;                        // hk_shape.attn_splits
+    float scale;
+};
+// Scratch of the call, and whether its launches stay within what a launch can hold.
+size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits);
+bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits);
+// Attention of T query tokens a request over the cache, and over the nodes' own rows (see kv_attn_kernel.h).
+hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s);
+
 }  // namespace hk

@@ -1,0 +1,110 @@
+// Attention over the paged K/V cache: the launch of the streaming kernel (kv_attn_kernel.h) in the cache's format, and the
+// merge of the pieces that a request's tokens were cut into.
+#include "kv_attn_kernel.h"
+
+namespace hk {
+namespace kvattn {
+namespace {
+
+constexpr int kMergeBatch = 8;
+
+// Joins the pieces of a row: one wavefront each, DH / 64 elements a lane.
+template <int DH, int DT>
+__global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
+{
+    typedef typename Elem<DT>::T elem_t;
+    constexpr int E = DH / 64;
+    const int lane = threadIdx.x & 63;
+    const int R = p.T * p.g;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= (int64_t)p.B * p.c.Hkv * R) return;
+    const int row = uniform((int)(id % R)), h = uniform((int)(id / R % p.c.Hkv)), r = uniform((int)(id / R / p.c.Hkv));
+    const int64_t C = piece_length(p, lane);
+    int n;
+    const int x0 = first_piece(p, C, r, lane, n);
+    const int nodes = nodes_of(p, r);
+    if (n == 1 || row >= nodes * p.g) return;              // its only piece has written it, or there is none
+    const int64_t slot0 = ((int64_t)x0 * p.c.Hkv + h) * R + row, step = (int64_t)p.c.Hkv * R;
+    const float *ml = p.partial + p.slots * DH;
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 64) top = fmaxf(top, ml[2 * (slot0 + i * step)]);
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float l = 0.f, o[E] = {};
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        float w = 0.f, lw = 0.f;
+        if (i0 + lane < n) {
+            const float2 v = *reinterpret_cast<const float2 *>(ml + 2 * (slot0 + (i0 + lane) * step));
+            w = __builtin_amdgcn_exp2f(v.x - ref);
+            lw = w * v.y;
+        }
+        for (int off = 32; off > 0; off >>= 1) lw += __shfl_xor(lw, off, 64);
+        l += lw;
+        const int upto = n - i0 < 64 ? n - i0 : 64;
+        for (int i = 0; i < upto; i += kMergeBatch) {      // every load of a batch on its way before the first use
+            float v[kMergeBatch][E], wi[kMergeBatch];
+#pragma unroll
+            for (int b = 0; b < kMergeBatch; ++b) {
+                const int at = i + b < upto ? i + b : i;   // a piece that fills the batch: read, not used
+                wi[b] = __shfl(w, i + b, 64);
+                const float *src = p.partial + (slot0 + (i0 + at) * step) * DH + lane * E;
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[b][e] = src[e];
+            }
+#pragma unroll
+            for (int b = 0; b < kMergeBatch; ++b)
+                if (i + b < upto) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(wi[b], v[b][e], o[e]);
+                }
+        }
+    }
+    // n > 1: the request has tokens, so every row of it sees some
+    elem_t *dst = static_cast<elem_t *>(p.out) + (((int64_t)r * p.T + row / p.g) * p.H + h * p.g + row % p.g) * DH + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) dst[e] = (elem_t)(o[e] / l);
+}
+
+template <int DH, int DT>
+hipError_t launch_merge(const Params &p, int64_t rows, hipStream_t s)
+{
+    hipLaunchKernelGGL((kv_merge_kernel<DH, DT>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace kvattn
+
+size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits)
+{
+    return (size_t)kvattn::plan(B, T, H, Hkv, head_dim, total_tokens, splits).partial_floats;
+}
+bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits)
+{
+    const kvattn::Plan pl = kvattn::plan(B, T, H, Hkv, head_dim, total_tokens, splits);
+    return pl.groups <= kvattn::kMostGroups && B * Hkv * pl.rows <= 4 * kvattn::kMostGroups;
+}
+
+hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s)
+{
+    using namespace kvattn;
+    if (a.B <= 0) return hipSuccess;
+    const Plan pl = plan(a.B, a.T, a.H, a.c.Hkv, a.head_dim, a.total_tokens, a.splits);
+    Params p;
+    p.c = a.c;
+    p.K_regen = a.K_regen; p.V_regen = a.V_regen; p.q = a.q; p.k = a.k; p.v = a.v;
+    p.mask = a.mask; p.n_nodes = a.n_nodes; p.out = a.out; p.partial = a.partial;
+    p.slots = pl.pieces * a.c.Hkv * pl.rows;
+    p.B = a.B; p.T = a.T; p.H = a.H; p.mask_stride = a.mask_stride; p.g = a.H / a.c.Hkv; p.row_groups = pl.row_groups;
+    p.extra = (int)pl.extra;
+    p.scale_log2e = a.scale * kLog2e;
+    const hipError_t e = a.format == kvfmt::k16     ? launch_16(p, pl, a.head_dim, a.dtype, s)
+                         : a.format == kvfmt::kInt8 ? launch_int8(p, pl, a.head_dim, a.dtype, s)
+                                                    : launch_e4m3(p, pl, a.head_dim, a.dtype, s);
+    if (e != hipSuccess || pl.extra <= 0) return e;
+    const int64_t rows = (int64_t)a.B * a.c.Hkv * pl.rows;
+    if (a.head_dim == 128) return a.dtype == 1 ? launch_merge<128, 1>(p, rows, s) : launch_merge<128, 0>(p, rows, s);
+    return a.dtype == 1 ? launch_merge<64, 1>(p, rows, s) : launch_merge<64, 0>(p, rows, s);
+}
+
+}  // namespace hk

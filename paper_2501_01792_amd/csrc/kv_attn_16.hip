@@ -1,0 +1,13 @@
+// The streaming kernel of the attention over a paged K/V cache whose pools hold the 16-bit storage type (kv_attn_kernel.h).
+#include "kv_attn_kernel.h"
+
+namespace hk {
+namespace kvattn {
+
+hipError_t launch_16(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s)
+{
+    return launch_format<kvfmt::k16>(p, pl, head_dim, dtype, s);
+}
+
+}  // namespace kvattn
+}  // namespace hk
