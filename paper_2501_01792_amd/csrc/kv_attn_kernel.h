@@ -114,18 +114,34 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void *base, uint
     const uint64_t lo = (uint32_t)uniform((int)(uint32_t)at), hi = (uint32_t)uniform((int)(uint32_t)(at >> 32));
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, uniform((int)bytes), 0x00020000);
 }
-// N bytes (4, 8, 16) at `off`, in the low words of the result.
+// N bytes (4, 8, 16) at `off`.
 template <int N>
-__device__ __forceinline__ u32x4_t fetch(__amdgpu_buffer_rsrc_t rs, int off)
+struct Words {
+    uint32_t w[N / 4];
+};
+template <int N>
+__device__ __forceinline__ Words<N> fetch(__amdgpu_buffer_rsrc_t rs, int off)
 {
-    if constexpr (N == 16) return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
-    else if constexpr (N == 8) {
-        const u32x2_t v = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
-        return u32x4_t{v[0], v[1], 0, 0};
-    } else {
-        return u32x4_t{(uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0), 0, 0, 0};
-    }
+    if constexpr (N == 16) return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+    else if constexpr (N == 8) return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
+    else return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0));
 }
+
+// The largest over the four lane groups of a row.
+__device__ __forceinline__ float max_over_groups(float v)
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    u2 s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    uint32_t a = s[0], b = s[1];
+    v = fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+    s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    a = s[0];
+    b = s[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+// How far the running maximum may lag behind, in the log2 domain: weights stay below 2^kLag.
+constexpr float kLag = 8.f;
 
 template <int DH, int DT, int FMT, int MT>
 struct Wave {
@@ -134,13 +150,17 @@ struct Wave {
     static constexpr int MDT = FMT == k16 ? DT : 0;        // type of the products over the cache
     typedef typename Elem<MDT>::V8 mvec8_t;
     static constexpr int KK = DH / 32, NI = DH / 16;
+    static constexpr int EB = FMT == k16 ? 2 : 1, RB = DH * EB;       // bytes of an element, of a row
+    static constexpr int VB = NI * EB;                     // bytes of a token that a lane reads of V
+    static constexpr int KR = FMT == k16 ? KK : KK / 2;    // 16-byte pieces of a token that a lane reads of K
 
     mvec8_t qf[MT][KK];
-    float qfac[MT];                                        // what the scores of a row are taken times
+    float qfac[MT];                                        // the power of two that a row's query was divided by
     float m[MT], l[MT];
     float4_t o[MT][NI];
     const elem_t *qrow[MT];                                // the query row of this lane's column
     uint64_t seen[MT];                                     // nodes that it sees
+    float scale;                                           // scale * log2(e)
     int g4, r16;
 
     // Reduction elements of product kk that this lane holds: 8 from here on.
@@ -149,33 +169,31 @@ struct Wave {
         return FMT == k16 ? kk * 32 + g4 * 8 : (kk >> 1) * 64 + g4 * 16 + (kk & 1) * 8;
     }
 
-    __device__ __forceinline__ void start(float scale_log2e)
+    __device__ __forceinline__ void start()
     {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             vec8_t raw[KK];
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) raw[kk] = *reinterpret_cast<const vec8_t *>(qrow[mt] + k_elem(kk));
-            float fac = 1.f;
+            qfac[mt] = 1.f;
             if constexpr (DT != MDT) {                     // bf16 -> fp16: the row's largest element between 1/2 and 1
                 float top = 0.f;
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) top = fmaxf(top, __builtin_fabsf((float)raw[kk][j]));
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                top = max_over_groups(top);
                 const int ex = top > 0.f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) qf[mt][kk][j] = (_Float16)__builtin_amdgcn_ldexpf((float)raw[kk][j], -ex);
-                fac = __builtin_amdgcn_ldexpf(1.f, ex);
+                qfac[mt] = __builtin_amdgcn_ldexpf(1.f, ex);
             } else {
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) qf[mt][kk] = raw[kk];
             }
-            qfac[mt] = fac * scale_log2e;
             m[mt] = -INFINITY;
             l[mt] = 0.f;
 #pragma unroll
@@ -183,202 +201,263 @@ struct Wave {
         }
     }
 
-    // Folds the scores t (log2 domain, -inf where masked) of row tile mt into (m, l, o) and returns 2^(t - m).
-    __device__ __forceinline__ void softmax(int mt, float (&t)[2][4])
+    // Moves the running maximum where a row's largest score `top` has left it behind; returns what scores are taken about
+    // (0 while the row has seen nothing: every weight is 2^-inf).
+    __device__ __forceinline__ float follow(int mt, float top)
     {
-        float top = t[0][0];
+        top = max_over_groups(top);
+        const bool behind = top > m[mt] + kLag;
+        if (__ballot(behind)) {
+            const float m_new = behind ? top : m[mt];
+            const float alpha = m_new == m[mt] ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
+            m[mt] = m_new;
+            l[mt] *= alpha;
 #pragma unroll
-        for (int u = 1; u < 8; ++u) top = fmaxf(top, t[u >> 2][u & 3]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = fmaxf(m[mt], top);
-        const float ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m[mt] - ref);
-        m[mt] = m_new;
-        l[mt] *= alpha;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) t[u >> 2][u & 3] = __builtin_amdgcn_exp2f(t[u >> 2][u & 3] - ref);
+            for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
+        }
+        return m[mt] == -INFINITY ? 0.f : m[mt];
     }
 
-    // V^T of 32 tokens: raw[s] is what this lane read of token slot s (16-bit elements) -> the NI operands.
-    static __device__ __forceinline__ void turn16(const u32x4_t (&raw)[8], u32x4_t (&vt)[NI])
+    // V^T of 32 tokens, of which this lane read raw[s] of token slot s: the operands of the elements in word w, two of 16 bits
+    // (as they are) or four codes (as fp16).
+    template <int N>
+    static __device__ __forceinline__ void turn16(const Words<N> (&raw)[8], int w, u32x4_t (&vt)[2])
     {
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                vt[i][s] = __builtin_amdgcn_perm(raw[2 * s + 1][i >> 1], raw[2 * s][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
+            for (int s = 0; s < 4; ++s) vt[i][s] = __builtin_amdgcn_perm(raw[2 * s + 1].w[w], raw[2 * s].w[w], i ? 0x07060302u : 0x05040100u);
     }
-    // The same from 8-bit codes, as fp16.
-    static __device__ __forceinline__ void turn8(const u32x4_t (&raw)[8], u32x4_t (&vt)[NI])
+    template <int N>
+    static __device__ __forceinline__ void turn8(const Words<N> (&raw)[8], int w, u32x4_t (&vt)[4])
     {
 #pragma unroll
-        for (int w = 0; w < NI / 4; ++w)
+        for (int q = 0; q < 2; ++q) {                      // token slots 4 q .. 4 q + 3
+            const uint32_t a = biased<FMT>(raw[4 * q].w[w]), b = biased<FMT>(raw[4 * q + 1].w[w]);
+            const uint32_t c = biased<FMT>(raw[4 * q + 2].w[w]), d = biased<FMT>(raw[4 * q + 3].w[w]);
+            const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+            const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+            const uint32_t e[4] = {__builtin_amdgcn_perm(cd0, ab0, 0x05040100u), __builtin_amdgcn_perm(cd0, ab0, 0x07060302u),
+                                   __builtin_amdgcn_perm(cd1, ab1, 0x05040100u), __builtin_amdgcn_perm(cd1, ab1, 0x07060302u)};
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {                  // token slots 4 q .. 4 q + 3, elements 4 w .. 4 w + 3
-                const uint32_t a = biased<FMT>(raw[4 * q][w]), b = biased<FMT>(raw[4 * q + 1][w]);
-                const uint32_t c = biased<FMT>(raw[4 * q + 2][w]), d = biased<FMT>(raw[4 * q + 3][w]);
-                const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
-                const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
-                const uint32_t e[4] = {__builtin_amdgcn_perm(cd0, ab0, 0x05040100u), __builtin_amdgcn_perm(cd0, ab0, 0x07060302u),
-                                       __builtin_amdgcn_perm(cd1, ab1, 0x05040100u), __builtin_amdgcn_perm(cd1, ab1, 0x07060302u)};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    vt[4 * w + j][2 * q] = __builtin_bit_cast(uint32_t, pair_f16<FMT, false>(e[j]));
-                    vt[4 * w + j][2 * q + 1] = __builtin_bit_cast(uint32_t, pair_f16<FMT, true>(e[j]));
-                }
+            for (int j = 0; j < 4; ++j) {
+                vt[j][2 * q] = __builtin_bit_cast(uint32_t, pair_f16<FMT, false>(e[j]));
+                vt[j][2 * q + 1] = __builtin_bit_cast(uint32_t, pair_f16<FMT, true>(e[j]));
             }
+        }
     }
 
-    // 32 cached tokens: rows n[j] of 16 at block offset base[j] (in rows of the pool), all wavefront-uniform.
+    // ---- 32 cached tokens, two 16s of which n[j] exist: where they are (wavefront-uniform) and what is on its way of them.
     struct Tokens {
-        const void *K[2], *V[2];                           // the 16 rows
+        const void *K[2], *V[2];
         const float *ks[2], *vs[2];
         int n[2];
     };
-    __device__ __forceinline__ void cached(const Tokens &tk)
+    Words<16> kraw[2][KR];
+    Words<VB> vraw[8];
+    float4_t ks[2], vs[2];
+
+    __device__ __forceinline__ void ask_k(const Tokens &tk)
     {
-        constexpr int EB = FMT == k16 ? 2 : 1, RB = DH * EB;          // bytes of an element, of a row
-        constexpr int VB = NI * EB;                                    // bytes of a token that a lane reads of V
-        float t[MT][2][4], ks[2][4], mant[2][4];
-        int e[2][4];
-        u32x4_t vraw[8];
-        mvec8_t kf[2][KK];
-        __amdgpu_buffer_rsrc_t vrs[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const __amdgpu_buffer_rsrc_t krs = rows_at(tk.K[j], tk.n[j] * RB);
-            vrs[j] = rows_at(tk.V[j], tk.n[j] * RB);
-            if constexpr (FMT == k16) {
+            const __amdgpu_buffer_rsrc_t rs = rows_at(tk.K[j], tk.n[j] * RB);
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    kf[j][kk] = __builtin_bit_cast(mvec8_t, fetch<16>(krs, r16 * RB + k_elem(kk) * EB));
-            } else {
+            for (int i = 0; i < KR; ++i) kraw[j][i] = fetch<16>(rs, r16 * RB + k_elem(FMT == k16 ? i : 2 * i) * EB);
+        }
+        if constexpr (FMT != k16) {
 #pragma unroll
-                for (int kp = 0; kp < KK / 2; ++kp) {
-                    u32x4_t raw = fetch<16>(krs, r16 * RB + k_elem(2 * kp));
+            for (int j = 0; j < 2; ++j) {
+                ks[j] = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.ks[j], 64), g4 * 16));
+                vs[j] = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.vs[j], 64), g4 * 16));
+            }
+        }
+    }
+    __device__ __forceinline__ void ask_v(const Tokens &tk)
+    {
+        const __amdgpu_buffer_rsrc_t rs[2] = {rows_at(tk.V[0], tk.n[0] * RB), rows_at(tk.V[1], tk.n[1] * RB)};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) vraw[s] = fetch<VB>(rs[s >> 2], (4 * g4 + (s & 3)) * RB + r16 * VB);
+    }
+    // Takes the tokens in; n as they were asked for.  `next`, when there is one, is asked for as registers fall free.
+    __device__ __forceinline__ void take(const int (&n)[2], const Tokens &next, bool more)
+    {
+        float4_t t[MT][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            mvec8_t kf[KK];
+#pragma unroll
+            for (int i = 0; i < KR; ++i) {
+                if constexpr (FMT == k16) {
+                    kf[i] = __builtin_bit_cast(mvec8_t, kraw[j][i]);
+                } else {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const uint32_t b = biased<FMT>(raw[w]);
+                        const uint32_t b = biased<FMT>(kraw[j][i].w[w]);
                         const half2_t lo = pair_f16<FMT, false>(b), hi = pair_f16<FMT, true>(b);
-                        mvec8_t &f = kf[j][2 * kp + (w >> 1)];
+                        mvec8_t &f = kf[2 * i + (w >> 1)];
                         const int at = 4 * (w & 1);
                         f[at] = lo[0]; f[at + 1] = lo[1]; f[at + 2] = hi[0]; f[at + 3] = hi[1];
                     }
                 }
             }
-        }
 #pragma unroll
-        for (int s = 0; s < 8; ++s) vraw[s] = fetch<VB>(vrs[s >> 2], (4 * g4 + (s & 3)) * RB + r16 * VB);
+            for (int mt = 0; mt < MT; ++mt) {
+                t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf[kk], qf[mt][kk], t[mt][j]);
+            }
+        }
+        // 8 bits: t = score * scale log2(e) + log2(vs), and the denominator's factor 1 / vs
+        float4_t inv[2];
         if constexpr (FMT != k16) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float4_t a = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.ks[j], 64), g4 * 16));
-                const float4_t b = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.vs[j], 64), g4 * 16));
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    ks[j][i] = a[i];
-                    const float v = b[i] < kLeastScale ? kLeastScale : b[i];
-                    const bool in = 4 * g4 + i < tk.n[j];
-                    mant[j][i] = in ? __builtin_amdgcn_frexp_mantf(v) : 0.f;
-                    e[j][i] = in ? __builtin_amdgcn_frexp_expf(v) : 0;
+                    const float kq = ks[j][i] * scale;
+                    const float v = vs[j][i] < kLeastScale ? kLeastScale : vs[j][i];
+                    const float lv = __builtin_amdgcn_logf(v);
+                    inv[j][i] = __builtin_amdgcn_rcpf(v);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        const float s = DT != MDT ? t[mt][j][i] * qfac[mt] : t[mt][j][i];
+                        t[mt][j][i] = __builtin_fmaf(s, kq, lv);
+                    }
                 }
-            }
         }
+        if (n[0] + n[1] < kTileTokens) {                   // tokens that do not exist
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float4_t s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk) s = Elem<MDT>::mfma_16x16x32(kf[j][kk], qf[mt][kk], s);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float v = s[i] * qfac[mt];
-                    if constexpr (FMT != k16) v = __builtin_fmaf(v, ks[j][i], (float)e[j][i]);
-                    t[mt][j][i] = 4 * g4 + i < tk.n[j] ? v : -INFINITY;
+                    const bool in = 4 * g4 + i < n[j];
+                    if constexpr (FMT != k16) inv[j][i] = in ? inv[j][i] : 0.f;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = in ? t[mt][j][i] : -INFINITY;
                 }
-            }
-        u32x4_t vt[NI];
-        if constexpr (FMT == k16) turn16(vraw, vt);
-        else turn8(vraw, vt);
+        }
+        if (more) ask_k(next);
+        __builtin_amdgcn_sched_barrier(0);
+        mvec8_t pf[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            softmax(mt, t[mt]);
-            mvec8_t pf;
+            float top = t[mt][0][0];
+#pragma unroll
+            for (int u = 1; u < 8; ++u) top = fmaxf(top, t[mt][u >> 2][u & 3]);
+            const float ref = follow(mt, FMT == k16 ? top * scale : top);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const float w = t[mt][u >> 2][u & 3];
-                if constexpr (FMT == k16) {
-                    l[mt] += w;
-                    pf[u] = (typename Elem<MDT>::T)w;
-                } else {
-                    l[mt] += __builtin_amdgcn_ldexpf(w, -e[u >> 2][u & 3]);
-                    pf[u] = (_Float16)(w * mant[u >> 2][u & 3]);
-                }
+                const float x = t[mt][u >> 2][u & 3];
+                const float w = __builtin_amdgcn_exp2f(FMT == k16 ? __builtin_fmaf(x, scale, -ref) : x - ref);
+                l[mt] = FMT == k16 ? l[mt] + w : __builtin_fmaf(w, inv[u >> 2][u & 3], l[mt]);
+                pf[mt][u] = (typename Elem<MDT>::T)w;
+            }
+        }
+        constexpr int G = FMT == k16 ? 2 : 4;
+#pragma unroll
+        for (int w = 0; w < NI / G; ++w) {
+            u32x4_t vt[G];
+            if constexpr (FMT == k16) turn16(vraw, w, vt);
+            else turn8(vraw, w, vt);
+            if (w == NI / G - 1) {                         // the last of vraw has been read
+                __builtin_amdgcn_sched_barrier(0);
+                if (more) ask_v(next);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int i = 0; i < NI; ++i) o[mt][i] = Elem<MDT>::mfma_16x16x32(__builtin_bit_cast(mvec8_t, vt[i]), pf, o[mt][i]);
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    o[mt][G * w + i] = Elem<MDT>::mfma_16x16x32(__builtin_bit_cast(mvec8_t, vt[i]), pf[mt], o[mt][G * w + i]);
         }
     }
 
-    // 32 nodes from node `first` on: K, V point at the first one's row, rows are `pitch` bytes apart, n of them exist.
+    // ---- 32 nodes from node `first` on: K, V point at the first one's row, rows are `pitch` bytes apart, n of them exist.
     __device__ __forceinline__ void drafted(const elem_t *K, const elem_t *V, int pitch, int first, int n)
     {
-        float t[MT][2][4];
-        vec8_t kf[2][KK];
-        u32x4_t vraw[8], vt[NI];
         const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * pitch + DH * 2 : 0;
-        const __amdgpu_buffer_rsrc_t krs = rows_at(K, bytes), vrs = rows_at(V, bytes);
+        float4_t t[MT][2];
+        {
+            const __amdgpu_buffer_rsrc_t rs = rows_at(K, bytes);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j) {
+                vec8_t kf[KK];
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-                kf[j][kk] = __builtin_bit_cast(vec8_t, fetch<16>(krs, (16 * j + r16) * pitch + (kk * 32 + g4 * 8) * 2));
+                for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(vec8_t, fetch<16>(rs, (16 * j + r16) * pitch + (kk * 32 + g4 * 8) * 2));
 #pragma unroll
-        for (int s = 0; s < 8; ++s) vraw[s] = fetch<NI * 2>(vrs, (16 * (s >> 2) + 4 * g4 + (s & 3)) * pitch + r16 * NI * 2);
+                for (int mt = 0; mt < MT; ++mt) {
+                    t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk)
+                        t[mt][j] = Elem<DT>::mfma_16x16x32(kf[kk], *reinterpret_cast<const vec8_t *>(qrow[mt] + kk * 32 + g4 * 8), t[mt][j]);
+                }
+            }
+        }
+        Words<NI * 2> raw[8];
+        {
+            const __amdgpu_buffer_rsrc_t rs = rows_at(V, bytes);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) raw[s] = fetch<NI * 2>(rs, (16 * (s >> 2) + 4 * g4 + (s & 3)) * pitch + r16 * NI * 2);
+        }
         // A weight of zero does not take an infinity or a NaN out of the product: such elements are zeros there and reach
         // the rows that see them on their own.
-        bool wild = false;
+        constexpr uint32_t ex = DT == 1 ? 0x7f80u : 0x7c00u;
+        uint32_t wild = 0;
 #pragma unroll
         for (int s = 0; s < 8; ++s)
 #pragma unroll
             for (int w = 0; w < NI / 2; ++w) {
-                constexpr uint32_t ex = DT == 1 ? 0x7f80u : 0x7c00u;
-                const bool lo = (vraw[s][w] & ex) == ex, hi = (vraw[s][w] >> 16 & ex) == ex;
-                wild = wild || lo || hi;
-                vraw[s][w] = (lo ? 0u : vraw[s][w] & 0xffffu) | (hi ? 0u : vraw[s][w] & 0xffff0000u);
+                const uint32_t x = raw[s].w[w];
+                wild |= ((x & ex) + (ex & -ex) & 0x8000u) | ((x >> 16 & ex) + (ex & -ex) & 0x8000u);   // an exponent of ones carries
             }
-        const bool any_wild = __ballot(wild) != 0;
-        turn16(vraw, vt);
+        const bool any_wild = __ballot(wild != 0) != 0;
+        if (any_wild) {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int w = 0; w < NI / 2; ++w) {
+                    const uint32_t x = raw[s].w[w];
+                    raw[s].w[w] = ((x & ex) == ex ? 0u : x & 0xffffu) | ((x >> 16 & ex) == ex ? 0u : x & 0xffff0000u);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+        vec8_t pf[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const float sc = qscale;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float4_t s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    s = Elem<DT>::mfma_16x16x32(kf[j][kk], *reinterpret_cast<const vec8_t *>(qrow[mt] + kk * 32 + g4 * 8), s);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t[mt][j][i] = (seen[mt] >> (first + 16 * j + 4 * g4 + i)) & 1 ? s[i] * sc : -INFINITY;
-            }
-            softmax(mt, t[mt]);
-            vec8_t pf;
+            float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                l[mt] += t[mt][u >> 2][u & 3];
-                pf[u] = (elem_t)t[mt][u >> 2][u & 3];
+                const float x = t[mt][u >> 2][u & 3] * scale;
+                t[mt][u >> 2][u & 3] = seen[mt] >> (first + 16 * (u >> 2) + 4 * g4 + (u & 3)) & 1 ? x : -INFINITY;
+                top = fmaxf(top, t[mt][u >> 2][u & 3]);
             }
+            const float ref = follow(mt, top);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) o[mt][i] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, vt[i]), pf, o[mt][i]);
-            if (any_wild) add_wild(V, pitch, first, n, mt, t[mt]);
+            for (int u = 0; u < 8; ++u) {
+                const float w = __builtin_amdgcn_exp2f(t[mt][u >> 2][u & 3] - ref);
+                t[mt][u >> 2][u & 3] = w;
+                l[mt] += w;
+                pf[mt][u] = (elem_t)w;
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < NI / 2; ++w) {
+            u32x4_t vt[2];
+            turn16(raw, w, vt);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    o[mt][2 * w + i] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, vt[i]), pf[mt], o[mt][2 * w + i]);
+        }
+        if (any_wild) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) add_wild(V, pitch, first, n, mt, t[mt]);
         }
     }
     // The infinities and NaN of V, node by node; t: the weights of this lane's row and tokens.
-    __device__ __forceinline__ void add_wild(const elem_t *V, int pitch, int first, int n, int mt, const float (&t)[2][4])
+    __device__ __forceinline__ void add_wild(const elem_t *V, int pitch, int first, int n, int mt, const float4_t (&t)[2])
     {
         for (int j = 0; j < n && j < kTileTokens; ++j) {
             float w = 0.f;
@@ -395,14 +474,50 @@ struct Wave {
                 for (int e = 0; e < 4; ++e) {
                     const float v = (float)row[(4 * g4 + e) * NI + i];
                     if (!(__builtin_fabsf(v) < INFINITY)) o[mt][i][e] += w * v;
+                    __builtin_amdgcn_sched_barrier(0);     // one by one: this path is for its results, not for its speed
                 }
         }
     }
-    float qscale;                                          // scale * log2(e)
 };
 
-template <int DH, int DT, int FMT, int MT>
-__global__ __launch_bounds__(kThreads) void kv_attn_kernel(Params p)
+// Table entries of the two 16s of the tile at token t (the last tile's second 16 may not exist: the first's entry stands in).
+__device__ __forceinline__ void entries_of(const int32_t *__restrict__ tab, int t, int t_end, int blk_log2, int (&e)[2])
+{
+    e[0] = tab[t >> blk_log2];
+    e[1] = tab[(t + 16 < t_end ? t + 16 : t) >> blk_log2];
+}
+
+template <typename wave_t, int FMT>
+__device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_end, const int (&ent)[2], typename wave_t::Tokens &tk)
+{
+    const int blk = 1 << p.c.blk_log2;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int here = t_end - (t0 + 16 * j), t = here > 0 ? t0 + 16 * j : t0;
+        tk.n[j] = here < 0 ? 0 : here < 16 ? here : 16;
+        const int e = uniform(ent[j]);
+        bool act = FMT == k16 && e < 0;
+        int pb = e < 0 ? ~e : e;
+        if constexpr (FMT == k16) {
+            if ((act ? p.c.P_act : p.c.P_kv) <= 0) { act = !act; pb = 0; }       // a corrupt table cannot leave
+        }
+        const int P = act ? p.c.P_act : p.c.P_kv;                                // the pools
+        pb = pb < P ? pb : P - 1;
+        const int64_t row = (((int64_t)pb * p.c.Hkv + h) << p.c.blk_log2) + (t & (blk - 1));
+        tk.K[j] = static_cast<const char *>(act ? p.K_regen : p.c.K_pool) + row * wave_t::RB;
+        tk.V[j] = static_cast<const char *>(act ? p.V_regen : p.c.V_pool) + row * wave_t::RB;
+        if constexpr (FMT != k16) {
+            tk.ks[j] = p.c.K_scale + row;
+            tk.vs[j] = p.c.V_scale + row;
+        }
+    }
+}
+
+// Wavefronts of a SIMD that the registers are held to.
+constexpr int residency(int DH, int FMT, int MT) { return MT == 1 ? (DH == 64 ? 3 : 2) : MT == 2 ? 2 : DH == 64 && MT == 3 ? 2 : 1; }
+
+template <int DH, int DT, int FMT, int MT, bool TREE>
+__global__ __launch_bounds__(kThreads, residency(DH, FMT, MT)) void kv_attn_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
@@ -427,7 +542,17 @@ __global__ __launch_bounds__(kThreads) void kv_attn_kernel(Params p)
     wave_t w;
     w.g4 = lane >> 4;
     w.r16 = lane & 15;
-    w.qscale = p.scale_log2e;
+    w.scale = p.scale_log2e;
+    const int32_t *tab = p.c.block_table + (int64_t)r * p.c.max_blocks;
+    int tb = t_begin + wave * kTileTokens;                 // pieces begin at whole rounds: wavefront 0 takes the first tile
+    typename wave_t::Tokens tk;
+    int ent[2] = {0, 0};
+    if (tb < t_end) {                                      // the first tile is on its way before the queries
+        entries_of(tab, tb, t_end, p.c.blk_log2, ent);
+        tokens_at<wave_t, FMT>(p, h, tb, t_end, ent, tk);
+        w.ask_k(tk);
+        w.ask_v(tk);
+    }
     bool some[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -435,42 +560,21 @@ __global__ __launch_bounds__(kThreads) void kv_attn_kernel(Params p)
         row = row < nodes * p.g ? row : nodes * p.g - 1;   // works on the last row, stores nothing
         const int node = row / p.g;
         w.qrow[mt] = static_cast<const elem_t *>(p.q) + (((int64_t)r * p.T + node) * p.H + h * p.g + row % p.g) * DH;
-        w.seen[mt] = seen_by(p, r, node, nodes);
+        w.seen[mt] = TREE ? seen_by(p, r, node, nodes) : 0;
         some[mt] = len > 0 || w.seen[mt] != 0;
     }
-    w.start(p.scale_log2e);
+    w.start();
 
-    const int32_t *tab = p.c.block_table + (int64_t)r * p.c.max_blocks;
-    const int blk = 1 << p.c.blk_log2;
-    constexpr int RB = DH * (FMT == k16 ? 2 : 1);
-    int turn = t_begin / kTileTokens;                      // pieces begin at whole rounds: wavefront 0 takes the first tile
-    for (int tb = t_begin + wave * kTileTokens; tb < t_end; tb += kStep) {
-        typename wave_t::Tokens tk;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int t = tb + 16 * j < t_end ? tb + 16 * j : tb;      // its table entry exists
-            const int here = t_end - (tb + 16 * j);
-            tk.n[j] = here < 0 ? 0 : here < 16 ? here : 16;
-            int e = uniform(tab[t >> p.c.blk_log2]);
-            bool act = FMT == k16 && e < 0;
-            int pb = e < 0 ? ~e : e;
-            if constexpr (FMT == k16) {
-                if ((act ? p.c.P_act : p.c.P_kv) <= 0) { act = !act; pb = 0; }       // a corrupt table cannot leave
-            }
-            const int P = act ? p.c.P_act : p.c.P_kv;                                // the pools
-            pb = pb < P ? pb : P - 1;
-            const int64_t row = (((int64_t)pb * p.c.Hkv + h) << p.c.blk_log2) + (t & (blk - 1));
-            tk.K[j] = static_cast<const char *>(act ? p.K_regen : p.c.K_pool) + row * RB;
-            tk.V[j] = static_cast<const char *>(act ? p.V_regen : p.c.V_pool) + row * RB;
-            if constexpr (FMT != k16) {
-                tk.ks[j] = p.c.K_scale + row;
-                tk.vs[j] = p.c.V_scale + row;
-            }
-        }
-        w.cached(tk);
+    if (tb + kStep < t_end) entries_of(tab, tb + kStep, t_end, p.c.blk_log2, ent);
+    for (; tb < t_end; tb += kStep) {
+        const int n[2] = {tk.n[0], tk.n[1]};
+        const bool more = tb + kStep < t_end;
+        if (more) tokens_at<wave_t, FMT>(p, h, tb + kStep, t_end, ent, tk);
+        if (tb + 2 * kStep < t_end) entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
+        w.take(n, tk, more);
     }
-    if (p.k && piece + 1 == pieces) {
-        turn = (t_end - t_begin + kTileTokens - 1) / kTileTokens;
+    if (TREE && p.k && piece + 1 == pieces) {
+        const int turn = (t_end - t_begin + kTileTokens - 1) / kTileTokens;
         const int pitch = p.c.Hkv * DH * 2;
         for (int d = 0; d * kTileTokens < nodes; ++d) {
             if ((turn + d) % kWaves != wave) continue;
@@ -558,10 +662,11 @@ template <int DH, int DT, int FMT>
 hipError_t launch_as(const Params &p, const Plan &pl, hipStream_t s)
 {
     const dim3 grid((unsigned)pl.groups), block(kThreads);
-    if (pl.tiles == 1) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 1>), grid, block, 0, s, p);
-    else if (pl.tiles == 2) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 2>), grid, block, 0, s, p);
-    else if (pl.tiles == 3) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 3>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 4>), grid, block, 0, s, p);
+    if (pl.tiles == 1 && !p.k) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 1, false>), grid, block, 0, s, p);
+    else if (pl.tiles == 1) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 1, true>), grid, block, 0, s, p);
+    else if (pl.tiles == 2) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 2, true>), grid, block, 0, s, p);
+    else if (pl.tiles == 3) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 3, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 4, true>), grid, block, 0, s, p);
     return hipGetLastError();
 }
 

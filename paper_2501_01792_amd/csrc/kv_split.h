@@ -48,7 +48,7 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
         S = splits > 1 ? B * splits : 0;
     } else if (B * across < kWantGroups) {
         S = (kWantGroups + across - 1) / across - B;
-        const int64_t most = total_tokens / (2 * kStep);     // a piece has two rounds at least
+        const int64_t most = total_tokens / kStep;           // a piece has a round at least
         S = S < most ? S : most;
     }
     p.extra = S;
