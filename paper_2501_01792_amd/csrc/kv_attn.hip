@@ -1,5 +1,5 @@
-// Attention over the paged K/V cache: the launch of the streaming kernel (kv_attn_kernel.h) in the cache's format, and the
-// merge of the pieces that a request's tokens were cut into.
+// Attention over the paged K/V cache: the launch of its kernels (kv_attn_kernel.h, kv_attn_rows.h) in the cache's format, and
+// the merge of the pieces that a request's tokens were cut into.
 #include "kv_attn_kernel.h"
 
 namespace hk {
@@ -96,7 +96,7 @@ hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s)
     p.mask = a.mask; p.n_nodes = a.n_nodes; p.out = a.out; p.partial = a.partial;
     p.slots = pl.pieces * a.c.Hkv * pl.rows;
     p.B = a.B; p.T = a.T; p.H = a.H; p.mask_stride = a.mask_stride; p.g = a.H / a.c.Hkv; p.row_groups = pl.row_groups;
-    p.extra = (int)pl.extra;
+    p.extra = (int)pl.extra; p.pieces = (int)pl.pieces;
     p.scale_log2e = a.scale * kLog2e;
     const hipError_t e = a.format == kvfmt::k16     ? launch_16(p, pl, a.head_dim, a.dtype, s)
                          : a.format == kvfmt::kInt8 ? launch_int8(p, pl, a.head_dim, a.dtype, s)

@@ -1,5 +1,5 @@
-// The streaming kernel of the attention over a paged K/V cache whose pools hold the 16-bit storage type (kv_attn_kernel.h).
-#include "kv_attn_kernel.h"
+// The kernels of the attention over a paged K/V cache whose pools hold the 16-bit storage type.
+#include "kv_attn_launch.h"
 
 namespace hk {
 namespace kvattn {

@@ -1,5 +1,5 @@
-// The streaming kernel of the attention over a paged K/V cache whose pools hold int8 codes (kv_attn_kernel.h).
-#include "kv_attn_kernel.h"
+// The kernels of the attention over a paged K/V cache whose pools hold int8 codes.
+#include "kv_attn_launch.h"
 
 namespace hk {
 namespace kvattn {

@@ -5,7 +5,7 @@
 // over the request's cached tokens and the nodes that node i sees; one pass over K and V with a running m (the usual rescaling
 // of the sums where it grows), everything after the products in fp32.
 //
-// One wavefront takes 32 tokens at a time and all 16 MT rows of its tile; K and V are read once for all of them.
+// One wavefront takes 32 tokens at a time and 16 MT query rows.
 //   scores   S^T = K Q^T with mfma 16x16x32: lane (g4 = lane / 16, r16 = lane % 16) holds tokens 4 g4 .. 4 g4 + 3 of each 16 of
 //            query row r16.  The reduction index may be permuted, so a lane reads K in whole 16-byte pieces.
 //   weights  the four tokens a lane holds of both 16s are the 8 reduction elements of its lane group in
@@ -15,8 +15,9 @@
 //            2^(t + e - m) mant <= 1 for the running maximum m of t + e, so the weight keeps fp16's 11 bits whatever the
 //            scales are, and the denominator takes 2^(t + e - m) 2^-e, in fp32.  A bf16 query is brought to fp16 by a power of
 //            two of its row.
-// A workgroup's 4 wavefronts take the 32-token tiles of a piece in turn and join at the end in LDS.  A piece that is its
-// request's only one writes the output; the others leave (m, l, o) for the merge.
+// Up to 32 rows (kv_attn_kernel): a workgroup's 4 wavefronts take the 32-token tiles of a piece in turn, rows of K and V go from
+// memory to registers, and they join at the end in LDS.  More rows: kv_attn_rows.h.  A piece that is its request's only one
+// writes the output; the others leave (m, l, o) for the merge.
 #pragma once
 #include "hk_internal.h"
 #include "kv_format.h"
@@ -37,9 +38,14 @@ struct Params {
     void *out;
     float *partial;                                        // [slots, DH] sums, then [slots] (m, l)
     int64_t slots;
-    int B, T, H, mask_stride, g, row_groups, extra;
+    int B, T, H, mask_stride, g, row_groups, extra, pieces;
     float scale_log2e;
 };
+
+// The streaming kernel in a cache's format; a translation unit each.
+hipError_t launch_16(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
+hipError_t launch_int8(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
+hipError_t launch_e4m3(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -108,6 +114,35 @@ __device__ __forceinline__ uint64_t seen_by(const Params &p, int r, int i, int n
     return m & have;
 }
 
+// What a workgroup works on.
+struct Place {
+    int rg, h, x;                                          // row group, K/V head, piece of the line of all pieces
+    int r, pieces, nodes, len, t_begin, t_end;             // request, its pieces, nodes, tokens; the piece's tokens
+    bool last;                                             // the request's last piece, which takes the nodes, too
+};
+// false: there is nothing to do.  Row groups of a piece are 8 workgroups apart: on one XCD, whose L2 the rows then come from.
+__device__ __forceinline__ bool place(const Params &p, int lane, Place &a)
+{
+    const int per = 8 * p.row_groups, b = blockIdx.x;
+    a.rg = b % per >> 3;
+    const int xh = b / per * 8 + (b & 7);
+    if (xh >= p.pieces * p.c.Hkv) return false;
+    a.h = xh % p.c.Hkv;
+    a.x = xh / p.c.Hkv;
+    const int64_t C = piece_length(p, lane);
+    int r = a.x, piece = 0, pieces = 1;
+    if (p.extra > 0 && !locate(p, C, a.x, lane, r, piece, pieces)) return false;
+    a.r = uniform(r);
+    piece = uniform(piece);
+    a.pieces = uniform(pieces);
+    a.nodes = uniform(nodes_of(p, a.r));
+    a.len = uniform(length_of(p.c, a.r));
+    a.t_begin = piece == 0 ? 0 : (int)(piece * C);
+    a.last = piece + 1 == a.pieces;
+    a.t_end = a.last ? a.len : (int)(a.t_begin + C);
+    return true;
+}
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void *base, uint32_t bytes)
 {
     const uint64_t at = reinterpret_cast<uintptr_t>(base);
@@ -161,12 +196,30 @@ struct Wave {
     const elem_t *qrow[MT];                                // the query row of this lane's column
     uint64_t seen[MT];                                     // nodes that it sees
     float scale;                                           // scale * log2(e)
-    int g4, r16;
+    int g4, r16, some;                                     // some: bit mt: the row sees something
 
     // Reduction elements of product kk that this lane holds: 8 from here on.
     __device__ __forceinline__ int k_elem(int kk) const
     {
         return FMT == k16 ? kk * 32 + g4 * 8 : (kk >> 1) * 64 + g4 * 16 + (kk & 1) * 8;
+    }
+
+    // The query rows of this lane's columns, from `first_row` on (rows that there are not: the last one, which is not stored).
+    __device__ __forceinline__ void rows(const Params &p, const Place &at, int first_row, int lane, bool tree)
+    {
+        g4 = lane >> 4;
+        r16 = lane & 15;
+        scale = p.scale_log2e;
+        some = 0;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            int row = first_row + mt * 16 + r16;
+            row = row < at.nodes * p.g ? row : at.nodes * p.g - 1;
+            const int node = row / p.g;
+            qrow[mt] = static_cast<const elem_t *>(p.q) + (((int64_t)at.r * p.T + node) * p.H + at.h * p.g + row % p.g) * DH;
+            seen[mt] = tree ? seen_by(p, at.r, node, at.nodes) : 0;
+            some |= (at.len > 0 || seen[mt] != 0) << mt;
+        }
     }
 
     __device__ __forceinline__ void start()
@@ -216,6 +269,81 @@ struct Wave {
             for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
         }
         return m[mt] == -INFINITY ? 0.f : m[mt];
+    }
+
+    // Scores t (-inf where there is no token; 16 bits: before the scale; 8 bits: with the scale and log2(vs), inv = 1 / vs) ->
+    // the weights as the product with V takes them; the denominator.
+    __device__ __forceinline__ void weigh(int mt, const float4_t (&t)[2], const float4_t (&inv)[2], mvec8_t &pf)
+    {
+        float top = t[0][0];
+#pragma unroll
+        for (int u = 1; u < 8; ++u) top = fmaxf(top, t[u >> 2][u & 3]);
+        const float ref = follow(mt, FMT == k16 ? top * scale : top);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float x = t[u >> 2][u & 3];
+            const float w = __builtin_amdgcn_exp2f(FMT == k16 ? __builtin_fmaf(x, scale, -ref) : x - ref);
+            l[mt] = FMT == k16 ? l[mt] + w : __builtin_fmaf(w, inv[u >> 2][u & 3], l[mt]);
+            pf[u] = (typename Elem<MDT>::T)w;
+        }
+    }
+    // The same for the scores (before the scale) of the 32 nodes from `first` on, of which the row sees some; t becomes the weights.
+    __device__ __forceinline__ void weigh_nodes(int mt, float4_t (&t)[2], int first, vec8_t &pf)
+    {
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float x = t[u >> 2][u & 3] * scale;
+            t[u >> 2][u & 3] = seen[mt] >> (first + 16 * (u >> 2) + 4 * g4 + (u & 3)) & 1 ? x : -INFINITY;
+            top = fmaxf(top, t[u >> 2][u & 3]);
+        }
+        const float ref = follow(mt, top);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float w = __builtin_amdgcn_exp2f(t[u >> 2][u & 3] - ref);
+            t[u >> 2][u & 3] = w;
+            l[mt] += w;
+            pf[u] = (elem_t)w;
+        }
+    }
+    // The lane groups' parts of the denominators.
+    __device__ __forceinline__ void sum_denominators()
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            l[mt] += __shfl_xor(l[mt], 16, 64);
+            l[mt] += __shfl_xor(l[mt], 32, 64);
+        }
+    }
+    // The rows' results: to the output, or as a piece's.
+    __device__ __forceinline__ void store(const Params &p, const Place &at, int first_row) const
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int row = first_row + mt * 16 + r16;
+            if (row >= at.nodes * p.g) continue;
+            if (at.pieces == 1) {
+                elem_t *dst = static_cast<elem_t *>(p.out) + (qrow[mt] - static_cast<const elem_t *>(p.q));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    typedef elem_t vec_t __attribute__((ext_vector_type(NI)));
+                    vec_t v;
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) v[i] = some >> mt & 1 ? (elem_t)(o[mt][i][e] / l[mt]) : (elem_t)0.f;
+                    *reinterpret_cast<vec_t *>(dst + (4 * g4 + e) * NI) = v;
+                }
+            } else {
+                const int64_t slot = ((int64_t)at.x * p.c.Hkv + at.h) * ((int64_t)p.T * p.g) + row;
+                float *dst = p.partial + slot * DH;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int i = 0; i < NI; i += 4)
+                        *reinterpret_cast<float4_t *>(dst + (4 * g4 + e) * NI + i) =
+                            float4_t{o[mt][i][e], o[mt][i + 1][e], o[mt][i + 2][e], o[mt][i + 3][e]};
+                if (g4 == 0) *reinterpret_cast<float2 *>(p.partial + p.slots * DH + 2 * slot) = make_float2(m[mt], l[mt]);
+            }
+        }
     }
 
     // V^T of 32 tokens, of which this lane read raw[s] of token slot s: the operands of the elements in word w, two of 16 bits
@@ -341,19 +469,7 @@ struct Wave {
         __builtin_amdgcn_sched_barrier(0);
         mvec8_t pf[MT];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float top = t[mt][0][0];
-#pragma unroll
-            for (int u = 1; u < 8; ++u) top = fmaxf(top, t[mt][u >> 2][u & 3]);
-            const float ref = follow(mt, FMT == k16 ? top * scale : top);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float x = t[mt][u >> 2][u & 3];
-                const float w = __builtin_amdgcn_exp2f(FMT == k16 ? __builtin_fmaf(x, scale, -ref) : x - ref);
-                l[mt] = FMT == k16 ? l[mt] + w : __builtin_fmaf(w, inv[u >> 2][u & 3], l[mt]);
-                pf[mt][u] = (typename Elem<MDT>::T)w;
-            }
-        }
+        for (int mt = 0; mt < MT; ++mt) weigh(mt, t[mt], inv, pf[mt]);
         constexpr int G = FMT == k16 ? 2 : 4;
 #pragma unroll
         for (int w = 0; w < NI / G; ++w) {
@@ -424,23 +540,7 @@ struct Wave {
         }
         vec8_t pf[MT];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float x = t[mt][u >> 2][u & 3] * scale;
-                t[mt][u >> 2][u & 3] = seen[mt] >> (first + 16 * (u >> 2) + 4 * g4 + (u & 3)) & 1 ? x : -INFINITY;
-                top = fmaxf(top, t[mt][u >> 2][u & 3]);
-            }
-            const float ref = follow(mt, top);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float w = __builtin_amdgcn_exp2f(t[mt][u >> 2][u & 3] - ref);
-                t[mt][u >> 2][u & 3] = w;
-                l[mt] += w;
-                pf[mt][u] = (elem_t)w;
-            }
-        }
+        for (int mt = 0; mt < MT; ++mt) weigh_nodes(mt, t[mt], first, pf[mt]);
 #pragma unroll
         for (int w = 0; w < NI / 2; ++w) {
             u32x4_t vt[2];
@@ -514,10 +614,10 @@ __device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_
 }
 
 // Wavefronts of a SIMD that the registers are held to.
-constexpr int residency(int DH, int FMT, int MT) { return MT == 1 ? (DH == 64 ? 3 : 2) : MT == 2 ? 2 : DH == 64 && MT == 3 ? 2 : 1; }
+constexpr int residency(int DH, int MT) { return MT == 1 && DH == 64 ? 3 : 2; }
 
 template <int DH, int DT, int FMT, int MT, bool TREE>
-__global__ __launch_bounds__(kThreads, residency(DH, FMT, MT)) void kv_attn_kernel(Params p)
+__global__ __launch_bounds__(kThreads, residency(DH, MT)) void kv_attn_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
@@ -525,43 +625,22 @@ __global__ __launch_bounds__(kThreads, residency(DH, FMT, MT)) void kv_attn_kern
     __shared__ float join_ml[kWaves][MT * 16][2];
     __shared__ float4_t join_o[MT * NI * 64];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int rg = blockIdx.x % p.row_groups, xh = blockIdx.x / p.row_groups;
-    const int h = xh % p.c.Hkv, x = xh / p.c.Hkv;
-    const int64_t C = piece_length(p, lane);
-    int r = x, piece = 0, pieces = 1;
-    if (p.extra > 0 && !locate(p, C, x, lane, r, piece, pieces)) return;
-    r = uniform(r);
-    piece = uniform(piece);
-    pieces = uniform(pieces);
-    const int nodes = uniform(nodes_of(p, r));
-    const int first_row = rg * MT * 16;
-    if (first_row >= nodes * p.g) return;                  // rows of nodes that there are not
-    const int len = uniform(length_of(p.c, r));
-    const int t_begin = piece == 0 ? 0 : (int)(piece * C), t_end = piece + 1 < pieces ? (int)(t_begin + C) : len;
-
+    Place at;
+    if (!place(p, lane, at)) return;
+    const int first_row = at.rg * MT * 16;
+    if (first_row >= at.nodes * p.g) return;               // rows of nodes that there are not
     wave_t w;
-    w.g4 = lane >> 4;
-    w.r16 = lane & 15;
-    w.scale = p.scale_log2e;
-    const int32_t *tab = p.c.block_table + (int64_t)r * p.c.max_blocks;
-    int tb = t_begin + wave * kTileTokens;                 // pieces begin at whole rounds: wavefront 0 takes the first tile
+    w.rows(p, at, first_row, lane, TREE);
+    const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
+    const int t_end = at.t_end;
+    int tb = at.t_begin + wave * kTileTokens;              // pieces begin at whole rounds: wavefront 0 takes the first tile
     typename wave_t::Tokens tk;
     int ent[2] = {0, 0};
     if (tb < t_end) {                                      // the first tile is on its way before the queries
         entries_of(tab, tb, t_end, p.c.blk_log2, ent);
-        tokens_at<wave_t, FMT>(p, h, tb, t_end, ent, tk);
+        tokens_at<wave_t, FMT>(p, at.h, tb, t_end, ent, tk);
         w.ask_k(tk);
         w.ask_v(tk);
-    }
-    bool some[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        int row = first_row + mt * 16 + w.r16;
-        row = row < nodes * p.g ? row : nodes * p.g - 1;   // works on the last row, stores nothing
-        const int node = row / p.g;
-        w.qrow[mt] = static_cast<const elem_t *>(p.q) + (((int64_t)r * p.T + node) * p.H + h * p.g + row % p.g) * DH;
-        w.seen[mt] = TREE ? seen_by(p, r, node, nodes) : 0;
-        some[mt] = len > 0 || w.seen[mt] != 0;
     }
     w.start();
 
@@ -569,28 +648,27 @@ __global__ __launch_bounds__(kThreads, residency(DH, FMT, MT)) void kv_attn_kern
     for (; tb < t_end; tb += kStep) {
         const int n[2] = {tk.n[0], tk.n[1]};
         const bool more = tb + kStep < t_end;
-        if (more) tokens_at<wave_t, FMT>(p, h, tb + kStep, t_end, ent, tk);
+        if (more) tokens_at<wave_t, FMT>(p, at.h, tb + kStep, t_end, ent, tk);
         if (tb + 2 * kStep < t_end) entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
         w.take(n, tk, more);
     }
-    if (TREE && p.k && piece + 1 == pieces) {
-        const int turn = (t_end - t_begin + kTileTokens - 1) / kTileTokens;
+    if (TREE && p.k && at.last) {
+        const int turn = (t_end - at.t_begin + kTileTokens - 1) / kTileTokens;
         const int pitch = p.c.Hkv * DH * 2;
-        for (int d = 0; d * kTileTokens < nodes; ++d) {
+        for (int d = 0; d * kTileTokens < at.nodes; ++d) {
             if ((turn + d) % kWaves != wave) continue;
-            const int64_t at = (((int64_t)r * p.T + d * kTileTokens) * p.c.Hkv + h) * DH;
-            const int n = nodes - d * kTileTokens;
-            w.drafted(static_cast<const elem_t *>(p.k) + at, static_cast<const elem_t *>(p.v) + at, pitch, d * kTileTokens,
+            const int64_t from = (((int64_t)at.r * p.T + d * kTileTokens) * p.c.Hkv + at.h) * DH;
+            const int n = at.nodes - d * kTileTokens;
+            w.drafted(static_cast<const elem_t *>(p.k) + from, static_cast<const elem_t *>(p.v) + from, pitch, d * kTileTokens,
                       n < kTileTokens ? n : kTileTokens);
         }
     }
 
     // The wavefronts' results about their common maximum, added in the order of the wavefronts.
     float ref[MT];
+    w.sum_denominators();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        w.l[mt] += __shfl_xor(w.l[mt], 16, 64);
-        w.l[mt] += __shfl_xor(w.l[mt], 32, 64);
         if (w.g4 == 0) {
             join_ml[wave][mt * 16 + w.r16][0] = w.m[mt];
             join_ml[wave][mt * 16 + w.r16][1] = w.l[mt];
@@ -628,59 +706,8 @@ __global__ __launch_bounds__(kThreads, residency(DH, FMT, MT)) void kv_attn_kern
         }
         __syncthreads();
     }
-    if (wave != 0) return;
-
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int row = first_row + mt * 16 + w.r16;
-        if (row >= nodes * p.g) continue;
-        if (pieces == 1) {
-            elem_t *dst = static_cast<elem_t *>(p.out) + (w.qrow[mt] - static_cast<const elem_t *>(p.q));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                typedef elem_t vec_t __attribute__((ext_vector_type(NI)));
-                vec_t v;
-#pragma unroll
-                for (int i = 0; i < NI; ++i) v[i] = some[mt] ? (elem_t)(w.o[mt][i][e] / w.l[mt]) : (elem_t)0.f;
-                *reinterpret_cast<vec_t *>(dst + (4 * w.g4 + e) * NI) = v;
-            }
-        } else {
-            const int64_t slot = ((int64_t)x * p.c.Hkv + h) * ((int64_t)p.T * p.g) + row;
-            float *dst = p.partial + slot * DH;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < NI; i += 4)
-                    *reinterpret_cast<float4_t *>(dst + (4 * w.g4 + e) * NI + i) =
-                        float4_t{w.o[mt][i][e], w.o[mt][i + 1][e], w.o[mt][i + 2][e], w.o[mt][i + 3][e]};
-            if (w.g4 == 0) *reinterpret_cast<float2 *>(p.partial + p.slots * DH + 2 * slot) = make_float2(w.m[mt], w.l[mt]);
-        }
-    }
+    if (wave == 0) w.store(p, at, first_row);
 }
-
-template <int DH, int DT, int FMT>
-hipError_t launch_as(const Params &p, const Plan &pl, hipStream_t s)
-{
-    const dim3 grid((unsigned)pl.groups), block(kThreads);
-    if (pl.tiles == 1 && !p.k) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 1, false>), grid, block, 0, s, p);
-    else if (pl.tiles == 1) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 1, true>), grid, block, 0, s, p);
-    else if (pl.tiles == 2) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 2, true>), grid, block, 0, s, p);
-    else if (pl.tiles == 3) hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 3, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((kv_attn_kernel<DH, DT, FMT, 4, true>), grid, block, 0, s, p);
-    return hipGetLastError();
-}
-
-template <int FMT>
-hipError_t launch_format(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s)
-{
-    if (head_dim == 128) return dtype == 1 ? launch_as<128, 1, FMT>(p, pl, s) : launch_as<128, 0, FMT>(p, pl, s);
-    return dtype == 1 ? launch_as<64, 1, FMT>(p, pl, s) : launch_as<64, 0, FMT>(p, pl, s);
-}
-
-// One translation unit each.
-hipError_t launch_16(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
-hipError_t launch_int8(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
-hipError_t launch_e4m3(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
 
 }  // namespace kvattn
 }  // namespace hk

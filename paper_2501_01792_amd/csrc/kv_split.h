@@ -2,8 +2,9 @@
 // code, so that it can be checked on a CPU.
 //
 // Query rows: the T nodes of a request x the g = H / Hkv query heads of a K/V head, row = node * g + head, in tiles of 16 (the
-// matrix instruction's columns).  A wavefront holds up to kMaxTiles tiles; more rows take more workgroups (`row_groups`), equal
-// up to a tile.
+// matrix instruction's columns).  Up to two tiles, every wavefront of a workgroup holds all rows and the tokens are shared out
+// among them; more, and the wavefronts share the tokens and hold one or two tiles each (`shared`), in as many workgroups
+// (`row_groups`) as that takes.
 // Tokens: a request's tokens are cut into pieces of C, the same C for all, found on the device from the lengths: with S extra
 // pieces to give away, C = sum(len) / S rounded up to a step of the workgroup makes at most B + S of them.  S = 0: one piece per
 // request, whatever its length, and no merge.
@@ -22,12 +23,13 @@ namespace kvattn {
 constexpr int kTileTokens = 32;                      // tokens a wavefront takes at once
 constexpr int kWaves = 4;
 constexpr int kStep = kTileTokens * kWaves;          // tokens of a workgroup's round
-constexpr int kMaxTiles = 4;                         // tiles of 16 query rows in a wavefront
+constexpr int kMaxTiles = 2;                         // tiles of 16 query rows in a wavefront
 constexpr int kWantGroups = 1024;                    // workgroups that fill the chip: 256 compute units x 4
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
 struct Plan {
     int64_t rows;            // T * g
+    bool shared;             // the wavefronts of a workgroup share the tokens, not the rows
     int tiles, row_groups;   // tiles of a wavefront, workgroups that share a piece
     int64_t extra;           // S
     int64_t pieces;          // B + S: pieces of the launch (device: at most)
@@ -40,8 +42,10 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
     Plan p;
     p.rows = T * (H / Hkv);
     const int64_t all = (p.rows + 15) / 16;
-    p.row_groups = (int)((all + kMaxTiles - 1) / kMaxTiles);
-    p.tiles = (int)((all + p.row_groups - 1) / p.row_groups);
+    p.shared = all > kMaxTiles;
+    const int64_t wide = p.shared ? kWaves : 1;          // wavefronts that hold different rows
+    p.row_groups = (int)((all + wide * kMaxTiles - 1) / (wide * kMaxTiles));
+    p.tiles = (int)((all + wide * p.row_groups - 1) / (wide * p.row_groups));
     const int64_t across = Hkv * p.row_groups;
     int64_t S = 0;
     if (splits > 0) {
@@ -53,7 +57,7 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
     }
     p.extra = S;
     p.pieces = B + S;
-    p.groups = p.pieces * across;
+    p.groups = (p.pieces * Hkv + 7) / 8 * 8 * p.row_groups;
     p.partial_floats = S > 0 ? p.pieces * Hkv * p.rows * (head_dim + 2) : 0;
     return p;
 }

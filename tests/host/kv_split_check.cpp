@@ -26,8 +26,9 @@ int main()
         const int64_t bound = total + (rng() % 2 ? 0 : rng() % 100000);
         const int splits = rng() % 3 ? 0 : (int)(rng() % 65);
         const Plan p = plan(B, T, (int64_t)Hkv * g, Hkv, 128, bound, splits);
-        if (p.rows != T * g || p.tiles < 1 || p.tiles > kMaxTiles || (int64_t)p.tiles * p.row_groups * 16 < p.rows ||
-            (int64_t)p.tiles * (p.row_groups - 1) * 16 >= p.rows || p.pieces != B + p.extra || p.extra < 0) {
+        const int64_t held = (int64_t)p.tiles * 16 * (p.shared ? kWaves : 1);      // rows of a workgroup
+        if (p.rows != T * g || p.tiles < 1 || p.tiles > kMaxTiles || held * p.row_groups < p.rows || held * (p.row_groups - 1) >= p.rows ||
+            p.pieces != B + p.extra || p.extra < 0 || p.groups < p.pieces * Hkv * p.row_groups) {
             std::printf("plan: rows %ld tiles %d groups %d\n", (long)p.rows, p.tiles, p.row_groups);
             return 1;
         }
