@@ -1,6 +1,7 @@
 // Attention over the paged K/V cache: the launch of its kernels (kv_attn_kernel.h, kv_attn_rows.h) in the cache's format, and
 // the merge of the pieces that a request's tokens were cut into.
 #include "kv_attn_kernel.h"
+#include "kv_attn_rows.h"
 
 namespace hk {
 namespace kvattn {
@@ -65,10 +66,59 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
     for (int e = 0; e < E; ++e) dst[e] = (elem_t)(o[e] / l);
 }
 
+// Joins the parts of a unit that more than one range of kv_attn_rows.h holds: the workgroup of the range in which the unit's
+// second part lies.  A wavefront takes rows in turn, DH / 64 elements a lane.
 template <int DH, int DT>
-hipError_t launch_merge(const Params &p, int64_t rows, hipStream_t s)
+__global__ __launch_bounds__(256) void kv_rows_merge_kernel(Params p, int held)
 {
-    hipLaunchKernelGGL((kv_merge_kernel<DH, DT>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+    typedef typename Elem<DT>::T elem_t;
+    constexpr int E = DH / 64;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wg = blockIdx.x + 1;
+    const int64_t total = line_total(p, lane, held);
+    const int used = ranges_used(total, p.groups);
+    if (wg >= used) return;
+    const int64_t pos = ranges::range_begin(wg, total, used);
+    int64_t begin;
+    const int r = request_at(p, pos, lane, held, begin);
+    const Request rq = request(p, r, held);
+    const int unit = (int)ranges::quot(pos - begin, rq.tiles);
+    const int64_t first = begin + (int64_t)unit * rq.tiles;
+    if (first == pos || ranges::range_begin(wg - 1, total, used) > first) return;   // the unit begins here, or its second part came before
+    const int last = ranges::owner(first + rq.tiles - 1, total, used);
+    const int h = unit / rq.groups, row0 = unit % rq.groups * held;
+    const int rows = rq.nodes * p.g - row0 < held ? rq.nodes * p.g - row0 : held;
+    const float *ml = p.partial + p.slots * DH;
+    for (int i = wave; i < rows; i += 4) {
+        // the first part is that of range wg - 1, which begins the unit; the others do not
+        float m = -INFINITY, l = 0.f, o[E] = {};
+        for (int x = wg - 1; x <= last; ++x) {
+            const int64_t slot = (int64_t)(2 * x + (x == wg - 1)) * held + i;
+            const float2 v = *reinterpret_cast<const float2 *>(ml + 2 * slot);
+            const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
+            const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(v.x - ref);
+            const float *src = p.partial + slot * DH + lane * E;
+            l = l * a + v.y * b;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = o[e] * a + src[e] * b;
+            m = top;
+        }
+        const int row = row0 + i, node = row / p.g;
+        const bool some = rq.len > 0 || seen_by(p, r, node, rq.nodes) != 0;
+        elem_t *dst = static_cast<elem_t *>(p.out) + (((int64_t)r * p.T + node) * p.H + h * p.g + row % p.g) * DH + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[e] = some ? (elem_t)(o[e] / l) : (elem_t)0.f;
+    }
+}
+
+template <int DH, int DT>
+hipError_t launch_merge(const Params &p, const Plan &pl, hipStream_t s)
+{
+    if (pl.shared) {
+        hipLaunchKernelGGL((kv_rows_merge_kernel<DH, DT>), dim3((unsigned)(pl.groups - 1)), dim3(256), 0, s, p, 16 * kWaves * pl.tiles);
+    } else {
+        const int64_t rows = (int64_t)p.B * p.c.Hkv * pl.rows;
+        hipLaunchKernelGGL((kv_merge_kernel<DH, DT>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
+    }
     return hipGetLastError();
 }
 
@@ -94,17 +144,16 @@ hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s)
     p.c = a.c;
     p.K_regen = a.K_regen; p.V_regen = a.V_regen; p.q = a.q; p.k = a.k; p.v = a.v;
     p.mask = a.mask; p.n_nodes = a.n_nodes; p.out = a.out; p.partial = a.partial;
-    p.slots = pl.pieces * a.c.Hkv * pl.rows;
-    p.B = a.B; p.T = a.T; p.H = a.H; p.mask_stride = a.mask_stride; p.g = a.H / a.c.Hkv; p.row_groups = pl.row_groups;
-    p.extra = (int)pl.extra; p.pieces = (int)pl.pieces;
+    p.slots = pl.slots;
+    p.B = a.B; p.T = a.T; p.H = a.H; p.mask_stride = a.mask_stride; p.g = a.H / a.c.Hkv;
+    p.extra = (int)pl.extra; p.groups = (int)pl.groups;
     p.scale_log2e = a.scale * kLog2e;
     const hipError_t e = a.format == kvfmt::k16     ? launch_16(p, pl, a.head_dim, a.dtype, s)
                          : a.format == kvfmt::kInt8 ? launch_int8(p, pl, a.head_dim, a.dtype, s)
                                                     : launch_e4m3(p, pl, a.head_dim, a.dtype, s);
-    if (e != hipSuccess || pl.extra <= 0) return e;
-    const int64_t rows = (int64_t)a.B * a.c.Hkv * pl.rows;
-    if (a.head_dim == 128) return a.dtype == 1 ? launch_merge<128, 1>(p, rows, s) : launch_merge<128, 0>(p, rows, s);
-    return a.dtype == 1 ? launch_merge<64, 1>(p, rows, s) : launch_merge<64, 0>(p, rows, s);
+    if (e != hipSuccess || pl.slots <= 0) return e;
+    if (a.head_dim == 128) return a.dtype == 1 ? launch_merge<128, 1>(p, pl, s) : launch_merge<128, 0>(p, pl, s);
+    return a.dtype == 1 ? launch_merge<64, 1>(p, pl, s) : launch_merge<64, 0>(p, pl, s);
 }
 
 }  // namespace hk

@@ -38,7 +38,7 @@ struct Params {
     void *out;
     float *partial;                                        // [slots, DH] sums, then [slots] (m, l)
     int64_t slots;
-    int B, T, H, mask_stride, g, row_groups, extra, pieces;
+    int B, T, H, mask_stride, g, extra, groups;            // groups: workgroups of the launch
     float scale_log2e;
 };
 
@@ -116,17 +116,14 @@ __device__ __forceinline__ uint64_t seen_by(const Params &p, int r, int i, int n
 
 // What a workgroup works on.
 struct Place {
-    int rg, h, x;                                          // row group, K/V head, piece of the line of all pieces
-    int r, pieces, nodes, len, t_begin, t_end;             // request, its pieces, nodes, tokens; the piece's tokens
+    int h, x;                                              // K/V head, piece of the line of all pieces
+    int r, pieces, nodes, len, t_begin, t_end;             // request, its pieces, nodes, tokens; the piece's (the part's) tokens
     bool last;                                             // the request's last piece, which takes the nodes, too
 };
-// false: there is nothing to do.  Row groups of a piece are 8 workgroups apart: on one XCD, whose L2 the rows then come from.
+// false: there is nothing to do.
 __device__ __forceinline__ bool place(const Params &p, int lane, Place &a)
 {
-    const int per = 8 * p.row_groups, b = blockIdx.x;
-    a.rg = b % per >> 3;
-    const int xh = b / per * 8 + (b & 7);
-    if (xh >= p.pieces * p.c.Hkv) return false;
+    const int xh = blockIdx.x;
     a.h = xh % p.c.Hkv;
     a.x = xh / p.c.Hkv;
     const int64_t C = piece_length(p, lane);
@@ -137,9 +134,9 @@ __device__ __forceinline__ bool place(const Params &p, int lane, Place &a)
     a.pieces = uniform(pieces);
     a.nodes = uniform(nodes_of(p, a.r));
     a.len = uniform(length_of(p.c, a.r));
-    a.t_begin = piece == 0 ? 0 : (int)(piece * C);
+    a.t_begin = uniform(piece == 0 ? 0 : (int)(piece * C));
     a.last = piece + 1 == a.pieces;
-    a.t_end = a.last ? a.len : (int)(a.t_begin + C);
+    a.t_end = uniform(a.last ? a.len : (int)(a.t_begin + C));
     return true;
 }
 
@@ -175,6 +172,14 @@ __device__ __forceinline__ float max_over_groups(float v)
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
+// Waits until at most N of this wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(N <= 63, "vmcnt counts to 63");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
+}
+
 // How far the running maximum may lag behind, in the log2 domain: weights stay below 2^kLag.
 constexpr float kLag = 8.f;
 
@@ -188,6 +193,7 @@ struct Wave {
     static constexpr int EB = FMT == k16 ? 2 : 1, RB = DH * EB;       // bytes of an element, of a row
     static constexpr int VB = NI * EB;                     // bytes of a token that a lane reads of V
     static constexpr int KR = FMT == k16 ? KK : KK / 2;    // 16-byte pieces of a token that a lane reads of K
+    static constexpr int kTileLoads = 2 * KR + (FMT == k16 ? 0 : 4) + 8;
 
     mvec8_t qf[MT][KK];
     float qfac[MT];                                        // the power of two that a row's query was divided by
@@ -222,15 +228,23 @@ struct Wave {
         }
     }
 
+    // The queries are asked for before the first rows of K and V: a wait for the latter is then one for the former, too.
+    __device__ __forceinline__ void ask_q()
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) qf[mt][kk] = *reinterpret_cast<const mvec8_t *>(qrow[mt] + k_elem(kk));
+    }
     __device__ __forceinline__ void start()
     {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            vec8_t raw[KK];
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) raw[kk] = *reinterpret_cast<const vec8_t *>(qrow[mt] + k_elem(kk));
             qfac[mt] = 1.f;
             if constexpr (DT != MDT) {                     // bf16 -> fp16: the row's largest element between 1/2 and 1
+                vec8_t raw[KK];
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) raw[kk] = __builtin_bit_cast(vec8_t, qf[mt][kk]);
                 float top = 0.f;
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk)
@@ -243,9 +257,6 @@ struct Wave {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) qf[mt][kk][j] = (_Float16)__builtin_amdgcn_ldexpf((float)raw[kk][j], -ex);
                 qfac[mt] = __builtin_amdgcn_ldexpf(1.f, ex);
-            } else {
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk) qf[mt][kk] = raw[kk];
             }
             m[mt] = -INFINITY;
             l[mt] = 0.f;
@@ -254,31 +265,47 @@ struct Wave {
         }
     }
 
-    // Moves the running maximum where a row's largest score `top` has left it behind; returns what scores are taken about
-    // (0 while the row has seen nothing: every weight is 2^-inf).
-    __device__ __forceinline__ float follow(int mt, float top)
+    // Moves the running maxima where a row's largest score, top[mt] (this lane's part of it), has left them behind by more than
+    // kLag; ref: what scores are taken about (0 while the row has seen nothing: every weight is 2^-inf).
+    __device__ __forceinline__ void follow(float (&top)[MT], float (&ref)[MT])
     {
-        top = max_over_groups(top);
-        const bool behind = top > m[mt] + kLag;
-        if (__ballot(behind)) {
-            const float m_new = behind ? top : m[mt];
-            const float alpha = m_new == m[mt] ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
-            m[mt] = m_new;
-            l[mt] *= alpha;
+        bool behind[MT], any = false;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
+        for (int mt = 0; mt < MT; ++mt) {
+            top[mt] = max_over_groups(top[mt]);
+            behind[mt] = top[mt] > m[mt] + kLag;
+            any = any || behind[mt];
         }
-        return m[mt] == -INFINITY ? 0.f : m[mt];
+        if (__ballot(any)) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const float alpha = behind[mt] ? __builtin_amdgcn_exp2f(m[mt] - top[mt]) : 1.f;
+                m[mt] = behind[mt] ? top[mt] : m[mt];
+                l[mt] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) ref[mt] = m[mt] == -INFINITY ? 0.f : m[mt];
     }
 
-    // Scores t (-inf where there is no token; 16 bits: before the scale; 8 bits: with the scale and log2(vs), inv = 1 / vs) ->
-    // the weights as the product with V takes them; the denominator.
-    __device__ __forceinline__ void weigh(int mt, const float4_t (&t)[2], const float4_t (&inv)[2], mvec8_t &pf)
+    // Scores t: -inf where there is no token; 16 bits: before the scale; 8 bits: with the scale and log2(vs), inv = 1 / vs.
+    __device__ __forceinline__ void references(const float4_t (&t)[MT][2], float (&ref)[MT])
     {
-        float top = t[0][0];
+        float top[MT];
 #pragma unroll
-        for (int u = 1; u < 8; ++u) top = fmaxf(top, t[u >> 2][u & 3]);
-        const float ref = follow(mt, FMT == k16 ? top * scale : top);
+        for (int mt = 0; mt < MT; ++mt) {
+            top[mt] = t[mt][0][0];
+#pragma unroll
+            for (int u = 1; u < 8; ++u) top[mt] = fmaxf(top[mt], t[mt][u >> 2][u & 3]);
+            if constexpr (FMT == k16) top[mt] *= scale;
+        }
+        follow(top, ref);
+    }
+    // The weights as the product with V takes them, and their part in the denominator.
+    __device__ __forceinline__ void weigh(int mt, const float4_t (&t)[2], const float4_t (&inv)[2], float ref, mvec8_t &pf)
+    {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const float x = t[u >> 2][u & 3];
@@ -287,24 +314,30 @@ struct Wave {
             pf[u] = (typename Elem<MDT>::T)w;
         }
     }
-    // The same for the scores (before the scale) of the 32 nodes from `first` on, of which the row sees some; t becomes the weights.
-    __device__ __forceinline__ void weigh_nodes(int mt, float4_t (&t)[2], int first, vec8_t &pf)
+    // The same for the scores (before the scale) of the 32 nodes from `first` on, of which the rows see some; t becomes the weights.
+    __device__ __forceinline__ void weigh_nodes(float4_t (&t)[MT][2], int first, vec8_t (&pf)[MT])
     {
-        float top = -INFINITY;
+        float top[MT], ref[MT];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float x = t[u >> 2][u & 3] * scale;
-            t[u >> 2][u & 3] = seen[mt] >> (first + 16 * (u >> 2) + 4 * g4 + (u & 3)) & 1 ? x : -INFINITY;
-            top = fmaxf(top, t[u >> 2][u & 3]);
-        }
-        const float ref = follow(mt, top);
+        for (int mt = 0; mt < MT; ++mt) {
+            top[mt] = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float w = __builtin_amdgcn_exp2f(t[u >> 2][u & 3] - ref);
-            t[u >> 2][u & 3] = w;
-            l[mt] += w;
-            pf[u] = (elem_t)w;
+            for (int u = 0; u < 8; ++u) {
+                const float x = t[mt][u >> 2][u & 3] * scale;
+                t[mt][u >> 2][u & 3] = seen[mt] >> (first + 16 * (u >> 2) + 4 * g4 + (u & 3)) & 1 ? x : -INFINITY;
+                top[mt] = fmaxf(top[mt], t[mt][u >> 2][u & 3]);
+            }
         }
+        follow(top, ref);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float w = __builtin_amdgcn_exp2f(t[mt][u >> 2][u & 3] - ref[mt]);
+                t[mt][u >> 2][u & 3] = w;
+                l[mt] += w;
+                pf[mt][u] = (elem_t)w;
+            }
     }
     // The lane groups' parts of the denominators.
     __device__ __forceinline__ void sum_denominators()
@@ -315,14 +348,14 @@ struct Wave {
             l[mt] += __shfl_xor(l[mt], 32, 64);
         }
     }
-    // The rows' results: to the output, or as a piece's.
-    __device__ __forceinline__ void store(const Params &p, const Place &at, int first_row) const
+    // The rows' results: to the output (`whole`: all tokens of theirs), or as a part's, row i in slot slot0 + i.
+    __device__ __forceinline__ void store(const Params &p, const Place &at, int first_row, bool whole, int64_t slot0) const
     {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int row = first_row + mt * 16 + r16;
             if (row >= at.nodes * p.g) continue;
-            if (at.pieces == 1) {
+            if (whole) {
                 elem_t *dst = static_cast<elem_t *>(p.out) + (qrow[mt] - static_cast<const elem_t *>(p.q));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -333,7 +366,7 @@ struct Wave {
                     *reinterpret_cast<vec_t *>(dst + (4 * g4 + e) * NI) = v;
                 }
             } else {
-                const int64_t slot = ((int64_t)at.x * p.c.Hkv + at.h) * ((int64_t)p.T * p.g) + row;
+                const int64_t slot = slot0 + row;
                 float *dst = p.partial + slot * DH;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -468,8 +501,10 @@ struct Wave {
         if (more) ask_k(next);
         __builtin_amdgcn_sched_barrier(0);
         mvec8_t pf[MT];
+        float ref[MT];
+        references(t, ref);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) weigh(mt, t[mt], inv, pf[mt]);
+        for (int mt = 0; mt < MT; ++mt) weigh(mt, t[mt], inv, ref[mt], pf[mt]);
         constexpr int G = FMT == k16 ? 2 : 4;
 #pragma unroll
         for (int w = 0; w < NI / G; ++w) {
@@ -539,8 +574,7 @@ struct Wave {
                 }
         }
         vec8_t pf[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) weigh_nodes(mt, t[mt], first, pf[mt]);
+        weigh_nodes(t, first, pf);
 #pragma unroll
         for (int w = 0; w < NI / 2; ++w) {
             u32x4_t vt[2];
@@ -627,30 +661,35 @@ __global__ __launch_bounds__(kThreads, residency(DH, MT)) void kv_attn_kernel(Pa
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     Place at;
     if (!place(p, lane, at)) return;
-    const int first_row = at.rg * MT * 16;
-    if (first_row >= at.nodes * p.g) return;               // rows of nodes that there are not
+    constexpr int first_row = 0;
+    if (at.nodes <= 0) return;                             // no rows
     wave_t w;
     w.rows(p, at, first_row, lane, TREE);
+    w.ask_q();
     const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
     const int t_end = at.t_end;
     int tb = at.t_begin + wave * kTileTokens;              // pieces begin at whole rounds: wavefront 0 takes the first tile
     typename wave_t::Tokens tk;
     int ent[2] = {0, 0};
-    if (tb < t_end) {                                      // the first tile is on its way before the queries
+    if (tb < t_end) {
         entries_of(tab, tb, t_end, p.c.blk_log2, ent);
         tokens_at<wave_t, FMT>(p, at.h, tb, t_end, ent, tk);
         w.ask_k(tk);
         w.ask_v(tk);
-    }
-    w.start();
-
-    if (tb + kStep < t_end) entries_of(tab, tb + kStep, t_end, p.c.blk_log2, ent);
-    for (; tb < t_end; tb += kStep) {
-        const int n[2] = {tk.n[0], tk.n[1]};
-        const bool more = tb + kStep < t_end;
-        if (more) tokens_at<wave_t, FMT>(p, at.h, tb + kStep, t_end, ent, tk);
-        if (tb + 2 * kStep < t_end) entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
-        w.take(n, tk, more);
+        w.start();
+        if (tb + kStep < t_end) entries_of(tab, tb + kStep, t_end, p.c.blk_log2, ent);
+        // Said once, in front of the loop: the queries are there.  Else every pass would wait for all that is on its way.
+        wait_loads<wave_t::kTileLoads>();
+        do {
+            const int n[2] = {tk.n[0], tk.n[1]};
+            const bool more = tb + kStep < t_end;
+            if (more) tokens_at<wave_t, FMT>(p, at.h, tb + kStep, t_end, ent, tk);
+            if (tb + 2 * kStep < t_end) entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
+            w.take(n, tk, more);
+            tb += kStep;
+        } while (tb < t_end);
+    } else {
+        w.start();
     }
     if (TREE && p.k && at.last) {
         const int turn = (t_end - at.t_begin + kTileTokens - 1) / kTileTokens;
@@ -706,7 +745,7 @@ __global__ __launch_bounds__(kThreads, residency(DH, MT)) void kv_attn_kernel(Pa
         }
         __syncthreads();
     }
-    if (wave == 0) w.store(p, at, first_row);
+    if (wave == 0) w.store(p, at, first_row, at.pieces == 1, ((int64_t)at.x * p.c.Hkv + at.h) * ((int64_t)p.T * p.g));
 }
 
 }  // namespace kvattn

@@ -5,26 +5,26 @@
 // rows of K and V (widening codes, turning V) costs as much as 16 to 32 query rows do.  So a wavefront makes a quarter of a
 // tile's operands and stores them in LDS in the order in which the matrix instructions read them, a lane's 16 bytes beside
 // its neighbour's; every wavefront reads them all.  Two buffers and one barrier a tile: while a tile is taken in, the next one's
-// operands are stored, and its successor's rows are on their way from memory.
-// The wavefronts never join: each has all tokens of its rows.
+// operands are stored, and the rows of the two behind that are on their way from memory.
+// The wavefronts never join: each has all tokens of its rows.  How the work is cut into ranges is in kv_split.h.
 #pragma once
 #include "kv_attn_kernel.h"
 
 namespace hk {
 namespace kvattn {
 
-// A tile's rows, two 16s of which n[j] exist: where they are (wavefront-uniform), `pitch` bytes apart.
+// A tile's rows, two 16s of which n0 and n1 exist: where they are (wavefront-uniform), `pitch` bytes apart.
 struct Rows {
-    const void *K[2], *V[2];
-    const float *ks[2], *vs[2];
-    int n[2], pitch;
+    const void *K0, *K1, *V0, *V1;
+    const float *ks0, *ks1, *vs0, *vs1;
+    int n0, n1, pitch;
 };
 
 template <int DH>
 struct Operands {
     u32x4_t k[2 * (DH / 32)][64];                          // [16s of tokens x products][lane]
     u32x4_t v[DH / 16][64];
-    float kq[kTileTokens], lv[kTileTokens], inv[kTileTokens];
+    float scales[4 * kTileTokens];                         // K's scale * softmax scale, log2 of V's, -, 1 / V's
     int wild;                                              // V of a tile of nodes holds infinities or NaN
 };
 
@@ -37,6 +37,7 @@ struct Part {
     static constexpr int NK = kCodes || DH == 64 ? 1 : 2;  // pieces of K, token slots of V (of the 8 a lane has) of a wavefront
     static constexpr int NV = !kCodes && DH == 128 ? 8 : 4;
     static constexpr bool kSplit = kCodes && DH == 64;     // two wavefronts take K, the others V
+    static constexpr int kLoads = (kSplit ? NK : NK + NV) + (kCodes ? 1 : 0);     // at least so many loads of a wavefront
     Words<16> kraw[NK];
     uint32_t vraw[NV];
     float sc;
@@ -52,7 +53,7 @@ struct Part {
         const int g4 = lane >> 4, r16 = lane & 15;
         if (!kSplit || wave < 2) {
             const int j = k_sixteen(wave);
-            const __amdgpu_buffer_rsrc_t rs = rows_at(j ? r.K[1] : r.K[0], bytes(r, j));
+            const __amdgpu_buffer_rsrc_t rs = rows_at(j ? r.K1 : r.K0, bytes(r, j));
 #pragma unroll
             for (int i = 0; i < NK; ++i) kraw[i] = fetch<16>(rs, r16 * r.pitch + k_piece(wave, i) * 64 + g4 * 16);
         }
@@ -60,29 +61,27 @@ struct Part {
 #pragma unroll
             for (int half = 0; half < NV / 4; ++half) {
                 const int q = NV == 8 ? half : v_quad(wave);
-                const __amdgpu_buffer_rsrc_t rs = rows_at(q ? r.V[1] : r.V[0], bytes(r, q));
+                const __amdgpu_buffer_rsrc_t rs = rows_at(q ? r.V1 : r.V0, bytes(r, q));
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
                     vraw[4 * half + s] = fetch<4>(rs, (4 * g4 + s) * r.pitch + r16 * VB + v_word(wave) * 4).w[0];
             }
         }
-        if constexpr (kCodes) {
-            if (wave == 3) {                               // a scale a lane: those of K in lanes 0 .. 31, of V in the others
-                const uintptr_t k0 = reinterpret_cast<uintptr_t>(r.ks[0]), k1 = reinterpret_cast<uintptr_t>(r.ks[1]);
-                const uintptr_t v0 = reinterpret_cast<uintptr_t>(r.vs[0]), v1 = reinterpret_cast<uintptr_t>(r.vs[1]);
-                const uintptr_t a = lane & 16 ? k1 : k0, b = lane & 16 ? v1 : v0;
-                sc = reinterpret_cast<const float *>(lane < 32 ? a : b)[r16];
-            }
+        if constexpr (kCodes) {                            // a scale a lane: those of K in lanes 0 .. 31, of V in the others
+            const uintptr_t k0 = reinterpret_cast<uintptr_t>(r.ks0), k1 = reinterpret_cast<uintptr_t>(r.ks1);
+            const uintptr_t v0 = reinterpret_cast<uintptr_t>(r.vs0), v1 = reinterpret_cast<uintptr_t>(r.vs1);
+            const uintptr_t a = lane & 16 ? k1 : k0, b = lane & 16 ? v1 : v0;
+            sc = reinterpret_cast<const float *>(lane < 32 ? a : b)[r16];
         }
     }
     static __device__ __forceinline__ uint32_t bytes(const Rows &r, int j)
     {
-        const int n = j ? r.n[1] : r.n[0];
+        const int n = j ? r.n1 : r.n0;
         return n > 0 ? (uint32_t)(n - 1) * r.pitch + RB : 0;
     }
 
-    // n: as the rows were asked for.
-    __device__ __forceinline__ void put(Operands<DH> &to, const int (&n)[2], int wave, int lane, float scale) const
+    // n0, n1: as the rows were asked for.
+    __device__ __forceinline__ void put(Operands<DH> &to, int n0, int n1, int wave, int lane, float scale) const
     {
         if (!kSplit || wave < 2) {
             const int j = k_sixteen(wave);
@@ -130,17 +129,14 @@ struct Part {
             }
         }
         if constexpr (kCodes) {
-            if (wave == 3) {                               // a token that does not exist: 0 s - inf, and no part of the denominator
-                const int tok = lane & 31;
-                const bool in = (tok & 15) < (tok < 16 ? n[0] : n[1]);
-                const float v = sc < kLeastScale ? kLeastScale : sc;
-                if (lane < 32) {
-                    to.kq[tok] = in ? sc * scale : 0.f;
-                } else {
-                    to.lv[tok] = in ? __builtin_amdgcn_logf(v) : -INFINITY;
-                    to.inv[tok] = in ? __builtin_amdgcn_rcpf(v) : 0.f;
-                }
-            }
+            // Every wavefront stores the same: a branch would part the products from what runs under them.  A token that does
+            // not exist: 0 s - inf, and no part of the denominator.
+            const int tok = lane & 31;
+            const bool in = (tok & 15) < (tok < 16 ? n0 : n1), of_k = lane < 32;
+            const float v = sc < kLeastScale ? kLeastScale : sc;
+            const float lv = in ? __builtin_amdgcn_logf(v) : -INFINITY, kq = in ? sc * scale : 0.f;
+            to.scales[lane] = of_k ? kq : lv;
+            to.scales[64 + lane] = in ? __builtin_amdgcn_rcpf(v) : 0.f;          // of V in the upper half
         }
     }
     // Infinities and NaN of V become zeros (16-bit rows); whether there were any.
@@ -168,136 +164,209 @@ __device__ __forceinline__ void meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// The tiles of a request's units on the line, and what the units are.
+struct Request {
+    int len, nodes, tiles, groups;
+    int64_t line;
+};
+__device__ __forceinline__ Request request(const Params &p, int r, int held)
+{
+    Request q;
+    q.len = length_of(p.c, r);
+    q.nodes = nodes_of(p, r);
+    q.tiles = unit_tiles(q.len, q.nodes, p.k != nullptr);
+    q.groups = unit_groups(q.nodes, p.g, held);
+    q.line = (int64_t)q.tiles * q.groups * p.c.Hkv;
+    return q;
+}
+__device__ __forceinline__ int64_t line_total(const Params &p, int lane, int held)
+{
+    int64_t sum = 0;
+    for (int r = lane; r < p.B; r += 64) sum += request(p, r, held).line;
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    return (int64_t)(uint32_t)uniform((int)(uint32_t)sum) | (int64_t)uniform((int)(sum >> 32)) << 32;
+}
+// The request that holds position x of the line (x < total), and where its tiles begin.
+__device__ __forceinline__ int request_at(const Params &p, int64_t x, int lane, int held, int64_t &begin)
+{
+    int64_t before = 0;
+    for (int r0 = 0; r0 < p.B; r0 += 64) {
+        const int64_t own = r0 + lane < p.B ? request(p, r0 + lane, held).line : 0;
+        int64_t upto = own;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t o = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += o;
+        }
+        const uint64_t in = __ballot(before + upto > x);
+        if (in) {
+            const int at = uniform(__builtin_ctzll(in));
+            begin = before + __shfl(upto - own, at, 64);
+            begin = (int64_t)(uint32_t)uniform((int)(uint32_t)begin) | (int64_t)uniform((int)(begin >> 32)) << 32;
+            return r0 + at;
+        }
+        before += __shfl(upto, 63, 64);
+    }
+    begin = 0;
+    return 0;
+}
+
 template <int DH, int DT, int FMT, int MT>
-__global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(Params p)
+__global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
     typedef typename wave_t::vec8_t vec8_t;
     typedef typename wave_t::mvec8_t mvec8_t;
-    constexpr int NI = wave_t::NI, KK = wave_t::KK, MDT = wave_t::MDT;
+    constexpr int NI = wave_t::NI, KK = wave_t::KK, MDT = wave_t::MDT, kHeld = kWaves * MT * 16;
     __shared__ Operands<DH> ops[2];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int64_t total = line_total(p, lane, kHeld);
+    const int used = ranges_used(total, p.groups);
+    // Workgroups go to the 8 XCDs in turn: neighbours on the line, which read the same rows, on one of them.
+    const int b = blockIdx.x, wg = p.groups % 8 == 0 ? (b & 7) * (p.groups / 8) + (b >> 3) : b;
+    if (wg >= used || total <= 0) return;
+    int64_t pos = ranges::range_begin(wg, total, used);
+    const int64_t end = ranges::range_begin(wg + 1, total, used);
+    int64_t begin;
     Place at;
-    if (!place(p, lane, at)) return;
-    const int group_rows = kWaves * MT * 16, group_first = at.rg * group_rows;
-    if (group_first >= at.nodes * p.g) return;             // rows of nodes that there are not
-    const int first_row = group_first + wave * MT * 16;
-    wave_t w;
-    w.rows(p, at, first_row, lane, true);
-    w.start();
+    at.r = request_at(p, pos, lane, kHeld, begin);
+    while (pos < end) {
+        const Request rq = request(p, at.r, kHeld);
+        if (pos >= begin + rq.line) {
+            begin += rq.line;
+            ++at.r;
+            continue;
+        }
+        // the part of a unit that this is: tiles [first, first + n) of rq.tiles
+        const int unit = (int)ranges::quot(pos - begin, rq.tiles);
+        const int first = (int)(pos - begin - (int64_t)unit * rq.tiles);
+        const int n = rq.tiles - first < end - pos ? rq.tiles - first : (int)(end - pos);
+        at.h = unit / rq.groups;
+        at.nodes = rq.nodes;
+        at.len = rq.len;
+        const int of_tokens = (rq.len + kTileTokens - 1) / kTileTokens;
+        at.t_begin = first < of_tokens ? first * kTileTokens : rq.len;
+        at.t_end = first + n < of_tokens ? (first + n) * kTileTokens : rq.len;
+        const int node_begin = (first > of_tokens ? first - of_tokens : 0) * kTileTokens;
+        const int node_end = p.k && first + n > of_tokens ? (first + n - of_tokens) * kTileTokens : 0;
+        const int group_first = unit % rq.groups * kHeld, first_row = group_first + wave * MT * 16;
+        pos += n;
 
-    const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
-    auto rows_of = [&](int t0, Rows &r) {
-        int ent[2];
-        entries_of(tab, t0, at.t_end, p.c.blk_log2, ent);
-        typename wave_t::Tokens tk;
-        tokens_at<wave_t, FMT>(p, at.h, t0, at.t_end, ent, tk);
+        wave_t w;
+        w.rows(p, at, first_row, lane, true);
+        w.ask_q();
+        const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
+        // Rows are asked for three tiles ahead (two wait in registers, in turn), their table entries four.
+        Part<DH, FMT> part[2];
+        int ent[2] = {0, 0}, t_ask = at.t_begin;
+        auto ask = [&](Part<DH, FMT> &to) {
+            if (t_ask >= at.t_end) return;
+            typename wave_t::Tokens tk;
+            tokens_at<wave_t, FMT>(p, at.h, t_ask, at.t_end, ent, tk);
+            t_ask += kTileTokens;
+            if (t_ask < at.t_end) entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
+            Rows r = {tk.K[0], tk.K[1], tk.V[0], tk.V[1], nullptr, nullptr, nullptr, nullptr, tk.n[0], tk.n[1], wave_t::RB};
+            if constexpr (FMT != k16) { r.ks0 = tk.ks[0]; r.ks1 = tk.ks[1]; r.vs0 = tk.vs[0]; r.vs1 = tk.vs[1]; }
+            to.ask(r, wave, lane);
+        };
+        auto put = [&](const Part<DH, FMT> &from, int t, Operands<DH> &to) {
+            const int here = at.t_end - t;
+            from.put(to, here < 16 ? here : 16, here < 16 ? 0 : here < 32 ? here - 16 : 16, wave, lane, w.scale);
+        };
+        // One tile: its successor's operands are made from `next`, which then waits for the tile two behind that.
+        auto tile = [&](int tb, const Operands<DH> &op, Operands<DH> &op_next, Part<DH, FMT> &next) {
+            // Operands are asked of LDS well ahead: K's before the next tile's are made, V's before the weights.
+            mvec8_t kf[2 * KK], vf[NI];
+            float4_t kq[2], lv[2], inv[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            r.K[j] = tk.K[j]; r.V[j] = tk.V[j]; r.n[j] = tk.n[j];
-            if constexpr (FMT != k16) { r.ks[j] = tk.ks[j]; r.vs[j] = tk.vs[j]; }
-        }
-        r.pitch = wave_t::RB;
-    };
-
-    Part<DH, FMT> part;
-    Rows ahead;                                            // of the tile whose rows are on their way
-    int tb = at.t_begin, cur = 0;
-    int n_cur[2] = {0, 0};
-    if (tb < at.t_end) {
-        rows_of(tb, ahead);
-        part.ask(ahead, wave, lane);
-        n_cur[0] = ahead.n[0];
-        n_cur[1] = ahead.n[1];
-        part.put(ops[0], ahead.n, wave, lane, w.scale);
-        if (tb + kTileTokens < at.t_end) {
-            rows_of(tb + kTileTokens, ahead);
-            part.ask(ahead, wave, lane);
-        }
-        meet();
-    }
-    for (; tb < at.t_end; tb += kTileTokens) {
-        const bool more = tb + kTileTokens < at.t_end;
-        int n_next[2] = {0, 0};
-        if (more) {
-            n_next[0] = ahead.n[0];
-            n_next[1] = ahead.n[1];
-            part.put(ops[cur ^ 1], ahead.n, wave, lane, w.scale);
-            if (tb + 2 * kTileTokens < at.t_end) {
-                rows_of(tb + 2 * kTileTokens, ahead);
-                part.ask(ahead, wave, lane);
+            for (int i = 0; i < 2 * KK; ++i) kf[i] = __builtin_bit_cast(mvec8_t, op.k[i][lane]);
+            if constexpr (FMT != k16) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    kq[j] = *reinterpret_cast<const float4_t *>(op.scales + 16 * j + 4 * w.g4);
+                    lv[j] = *reinterpret_cast<const float4_t *>(op.scales + 32 + 16 * j + 4 * w.g4);
+                    inv[j] = *reinterpret_cast<const float4_t *>(op.scales + 96 + 16 * j + 4 * w.g4);
+                }
             }
-        }
-        const Operands<DH> &op = ops[cur];
-        float4_t t[MT][2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                const mvec8_t kf = __builtin_bit_cast(mvec8_t, op.k[j * KK + kk][lane]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf, w.qf[mt][kk], t[mt][j]);
-            }
-        }
-        float4_t inv[2];
-        if constexpr (FMT != k16) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float4_t kq = *reinterpret_cast<const float4_t *>(op.kq + 16 * j + 4 * w.g4);
-                const float4_t lv = *reinterpret_cast<const float4_t *>(op.lv + 16 * j + 4 * w.g4);
-                inv[j] = *reinterpret_cast<const float4_t *>(op.inv + 16 * j + 4 * w.g4);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t[mt][j][i] = __builtin_fmaf(DT != MDT ? t[mt][j][i] * w.qfac[mt] : t[mt][j][i], kq[i], lv[i]);
-            }
-        } else if (n_cur[0] + n_cur[1] < kTileTokens) {
+            __builtin_amdgcn_sched_barrier(0);
+            put(next, tb + kTileTokens, op_next);              // behind the last tile: what nobody reads
+            float4_t t[MT][2];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int mt = 0; mt < MT; ++mt) t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = 4 * w.g4 + i < n_cur[j] ? t[mt][j][i] : -INFINITY;
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf[j * KK + kk], w.qf[mt][kk], t[mt][j]);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) vf[i] = __builtin_bit_cast(mvec8_t, op.v[i][lane]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (FMT != k16) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            t[mt][j][i] = __builtin_fmaf(DT != MDT ? t[mt][j][i] * w.qfac[mt] : t[mt][j][i], kq[j][i], lv[j][i]);
+            } else if (at.t_end - tb < kTileTokens) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = tb + 16 * j + 4 * w.g4 + i < at.t_end ? t[mt][j][i] : -INFINITY;
+            }
+            mvec8_t pf[MT];
+            float ref[MT];
+            w.references(t, ref);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {                  // one tile's products run under the next one's weights
+                w.weigh(mt, t[mt], inv, ref[mt], pf[mt]);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) w.o[mt][i] = Elem<MDT>::mfma_16x16x32(vf[i], pf[mt], w.o[mt][i]);
+            }
+            ask(next);
+            meet();                                            // the next tile is there, and this one's buffer is free
+        };
+        if (at.t_begin < at.t_end) {
+            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
+            ask(part[0]);
+            ask(part[1]);
+            w.start();
+            put(part[0], at.t_begin, ops[0]);
+            // Said once, in front of the loop: the queries are there.  Else every tile would wait for all that is on its way.
+            wait_loads<Part<DH, FMT>::kLoads>();
+            ask(part[0]);
+            meet();
+            int tb = at.t_begin;
+            do {
+                tile(tb, ops[0], ops[1], part[1]);
+                if (tb + kTileTokens < at.t_end) tile(tb + kTileTokens, ops[1], ops[0], part[0]);
+                tb += 2 * kTileTokens;
+            } while (tb < at.t_end);
+        } else {
+            w.start();
         }
-        mvec8_t pf[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) w.weigh(mt, t[mt], inv, pf[mt]);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const mvec8_t vf = __builtin_bit_cast(mvec8_t, op.v[i][lane]);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) w.o[mt][i] = Elem<MDT>::mfma_16x16x32(vf, pf[mt], w.o[mt][i]);
-        }
-        n_cur[0] = n_next[0];
-        n_cur[1] = n_next[1];
-        cur ^= 1;
-        meet();                                            // the next tile is there, and this one's buffer is free
-    }
 
-    if (p.k && at.last) {
         const int pitch = p.c.Hkv * DH * 2;
-        for (int first = 0; first < at.nodes; first += kTileTokens) {
-            const int64_t from = (((int64_t)at.r * p.T + first) * p.c.Hkv + at.h) * DH;
+        for (int node = node_begin; node < node_end && node < at.nodes; node += kTileTokens) {
+            const int64_t from = (((int64_t)at.r * p.T + node) * p.c.Hkv + at.h) * DH;
             const elem_t *K = static_cast<const elem_t *>(p.k) + from, *V = static_cast<const elem_t *>(p.v) + from;
-            const int n = at.nodes - first < kTileTokens ? at.nodes - first : kTileTokens;
-            Rows r;
-            r.K[0] = K; r.V[0] = V;
-            r.K[1] = reinterpret_cast<const char *>(K) + 16 * pitch;
-            r.V[1] = reinterpret_cast<const char *>(V) + 16 * pitch;
-            r.n[0] = n < 16 ? n : 16;
-            r.n[1] = n < 16 ? 0 : n - 16;
-            r.pitch = pitch;
+            const int here = at.nodes - node < kTileTokens ? at.nodes - node : kTileTokens;
+            const Rows r = {K, reinterpret_cast<const char *>(K) + 16 * pitch, V, reinterpret_cast<const char *>(V) + 16 * pitch,
+                            nullptr, nullptr, nullptr, nullptr, here < 16 ? here : 16, here < 16 ? 0 : here - 16, pitch};
             Part<DH, k16> nodes;
             nodes.ask(r, wave, lane);
-            if (threadIdx.x == 0) ops[cur].wild = 0;
+            if (threadIdx.x == 0) ops[0].wild = 0;
             meet();
-            if (nodes.template tame<DT>() && lane == 0) ops[cur].wild = 1;
-            nodes.put(ops[cur], r.n, wave, lane, 0.f);
+            if (nodes.template tame<DT>() && lane == 0) ops[0].wild = 1;
+            nodes.put(ops[0], r.n0, r.n1, wave, lane, 0.f);
             meet();
-            const Operands<DH> &op = ops[cur];
+            const Operands<DH> &op = ops[0];
             float4_t t[MT][2];
             vec8_t pf[MT];
 #pragma unroll
@@ -310,8 +379,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(Params p)
                         t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, op.k[j * KK + kk][lane]),
                                                            *reinterpret_cast<const vec8_t *>(w.qrow[mt] + kk * 32 + w.g4 * 8), t[mt][j]);
                 }
-                w.weigh_nodes(mt, t[mt], first, pf[mt]);
             }
+            w.weigh_nodes(t, node, pf);
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const vec8_t vf = __builtin_bit_cast(vec8_t, op.v[i][lane]);
@@ -320,13 +389,14 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(Params p)
             }
             if (uniform(op.wild)) {
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) w.add_wild(V, pitch, first, n, mt, t[mt]);
+                for (int mt = 0; mt < MT; ++mt) w.add_wild(V, pitch, node, here, mt, t[mt]);
             }
             meet();
         }
+        w.sum_denominators();
+        // a range has one part that does not begin its unit at most, and one that begins a unit and does not end it
+        w.store(p, at, first_row, n == rq.tiles, (int64_t)(2 * wg + (first == 0)) * kHeld - group_first);
     }
-    w.sum_denominators();
-    w.store(p, at, first_row);
 }
 
 }  // namespace kvattn

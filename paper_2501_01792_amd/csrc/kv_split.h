@@ -2,38 +2,44 @@
 // code, so that it can be checked on a CPU.
 //
 // Query rows: the T nodes of a request x the g = H / Hkv query heads of a K/V head, row = node * g + head, in tiles of 16 (the
-// matrix instruction's columns).  Up to two tiles, every wavefront of a workgroup holds all rows and the tokens are shared out
-// among them; more, and the wavefronts share the tokens and hold one or two tiles each (`shared`), in as many workgroups
-// (`row_groups`) as that takes.
-// Tokens: a request's tokens are cut into pieces of C, the same C for all, found on the device from the lengths: with S extra
-// pieces to give away, C = sum(len) / S rounded up to a step of the workgroup makes at most B + S of them.  S = 0: one piece per
-// request, whatever its length, and no merge.
+// matrix instruction's columns).
+//
+// Up to two tiles, every wavefront of a workgroup holds all rows and the tokens are shared out among them.  A request's tokens
+// are cut into pieces of C, the same C for all, found on the device from the lengths: with S extra pieces to give away, C =
+// sum(len) / S rounded up to a step of the workgroup makes at most B + S of them.  S = 0: one piece per request, whatever its
+// length, and no merge.
+//
+// More tiles, and the wavefronts of a workgroup share the tokens and hold one or two tiles each (`shared`).  Such work is
+// bound by arithmetic, so the compute units have to get equal shares of it, whatever the lengths and trees are: a unit is a row
+// group (the rows of a workgroup) of a K/V head of a request, it takes its tokens' and its nodes' tiles of 32 one after the other,
+// and the tiles of all units form a line that the workgroups, as many as are resident at once, cut into equal ranges.  A
+// workgroup leaves at most two units unfinished, the first and the last of its range.
 #pragma once
 #include <stdint.h>
 
-#if defined(__HIPCC__)
-#define HK_HOST_DEVICE __host__ __device__
-#else
-#define HK_HOST_DEVICE
-#endif
+#include "attn_ranges.h"
 
 namespace hk {
 namespace kvattn {
 
 constexpr int kTileTokens = 32;                      // tokens a wavefront takes at once
 constexpr int kWaves = 4;
-constexpr int kStep = kTileTokens * kWaves;          // tokens of a workgroup's round
+constexpr int kStep = kTileTokens * kWaves;          // tokens of a round of a workgroup whose wavefronts share them out
 constexpr int kMaxTiles = 2;                         // tiles of 16 query rows in a wavefront
 constexpr int kWantGroups = 1024;                    // workgroups that fill the chip: 256 compute units x 4
+constexpr int kLeastRange = 4;                       // tiles of a range at least
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
+
+// Workgroups of a compute unit that the registers of the shared form leave room for.
+HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 ? (tiles == 1 ? 4 : 3) : tiles == 1 ? 3 : 2; }
 
 struct Plan {
     int64_t rows;            // T * g
     bool shared;             // the wavefronts of a workgroup share the tokens, not the rows
-    int tiles, row_groups;   // tiles of a wavefront, workgroups that share a piece
+    int tiles;               // tiles of a wavefront
     int64_t extra;           // S
-    int64_t pieces;          // B + S: pieces of the launch (device: at most)
     int64_t groups;          // workgroups of the launch
+    int64_t slots;           // rows of unfinished results
     int64_t partial_floats;
 };
 
@@ -43,22 +49,31 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
     p.rows = T * (H / Hkv);
     const int64_t all = (p.rows + 15) / 16;
     p.shared = all > kMaxTiles;
-    const int64_t wide = p.shared ? kWaves : 1;          // wavefronts that hold different rows
-    p.row_groups = (int)((all + wide * kMaxTiles - 1) / (wide * kMaxTiles));
-    p.tiles = (int)((all + wide * p.row_groups - 1) / (wide * p.row_groups));
-    const int64_t across = Hkv * p.row_groups;
-    int64_t S = 0;
-    if (splits > 0) {
-        S = splits > 1 ? B * splits : 0;
-    } else if (B * across < kWantGroups) {
-        S = (kWantGroups + across - 1) / across - B;
-        const int64_t most = total_tokens / kStep;           // a piece has a round at least
-        S = S < most ? S : most;
+    p.extra = 0;
+    if (p.shared) {
+        p.tiles = all > kWaves ? 2 : 1;
+        const int64_t held = 16 * kWaves * p.tiles;
+        // tiles of the line at most: those of the tokens, a last one of each request that is not full, two of nodes
+        const int64_t line = (total_tokens / kTileTokens + 3 * B) * Hkv * ((p.rows + held - 1) / held);
+        const int64_t want = splits > 0 ? B * Hkv * splits : 256 * resident(head_dim, p.tiles);
+        const int64_t fit = (line + kLeastRange - 1) / kLeastRange;
+        p.groups = want < fit ? want : fit > 0 ? fit : 1;
+        p.slots = p.groups > 1 ? 2 * p.groups * held : 0;
+    } else {
+        p.tiles = (int)all;
+        int64_t S = 0;
+        if (splits > 0) {
+            S = splits > 1 ? B * splits : 0;
+        } else if (B * Hkv < kWantGroups) {
+            S = (kWantGroups + Hkv - 1) / Hkv - B;
+            const int64_t most = total_tokens / kStep;       // a piece has a round at least
+            S = S < most ? S : most;
+        }
+        p.extra = S;
+        p.groups = (B + S) * Hkv;
+        p.slots = S > 0 ? p.groups * p.rows : 0;
     }
-    p.extra = S;
-    p.pieces = B + S;
-    p.groups = (p.pieces * Hkv + 7) / 8 * 8 * p.row_groups;
-    p.partial_floats = S > 0 ? p.pieces * Hkv * p.rows * (head_dim + 2) : 0;
+    p.partial_floats = p.slots * (head_dim + 2);
     return p;
 }
 
@@ -68,6 +83,20 @@ HK_HOST_DEVICE inline int64_t piece_tokens(int64_t total, int64_t S)
     if (S <= 0) return int64_t(1) << 40;
     const int64_t C = (((uint64_t)total | (uint64_t)S) >> 32) == 0 ? (int64_t)(((uint32_t)total + (uint32_t)(S - 1)) / (uint32_t)S) : (total + S - 1) / S;
     return C < kStep ? kStep : (C + kStep - 1) / kStep * kStep;
+}
+
+// The shared form's line.  Tiles of a unit of a request (a request without tokens and nodes' rows of its own has an empty one:
+// its rows are written all the same), its row groups, and the ranges that take part when the line has `total` tiles.
+HK_HOST_DEVICE inline int unit_tiles(int len, int nodes, bool tree)
+{
+    const int n = (len + kTileTokens - 1) / kTileTokens + (tree ? (nodes + kTileTokens - 1) / kTileTokens : 0);
+    return n > 0 ? n : 1;
+}
+HK_HOST_DEVICE inline int unit_groups(int nodes, int g, int held) { return (nodes * g + held - 1) / held; }
+HK_HOST_DEVICE inline int ranges_used(int64_t total, int groups)
+{
+    const int64_t fit = (total + kLeastRange - 1) / kLeastRange;
+    return fit < groups ? (int)(fit > 0 ? fit : 1) : groups;
 }
 
 // Pieces of a request; one without tokens has one, which writes its output.
