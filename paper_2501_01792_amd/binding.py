@@ -590,7 +590,7 @@ class KvCache:
     """Handle of a paged K/V cache (hk_kv_cache): its tensors, kept alive, and the C struct that names them.  Made once by
     ``make_kv_cache``; the tensors are used where they are, so a change of their contents is seen by the next call."""
 
-    __slots__ = ("struct", "ref", "tensors", "device", "pool_dtype", "B", "n_kv_heads", "head_dim", "d_act", "shapes")
+    __slots__ = ("struct", "ref", "tensors", "device", "index", "pool_dtype", "B", "n_kv_heads", "head_dim", "d_act", "shapes")
 
 
 def make_kv_cache(K_pool, V_pool, block_table, seq_len, block_tokens, K_scale=None, V_scale=None, act_pool=None, n_act_used=None,
@@ -617,8 +617,10 @@ def make_kv_cache(K_pool, V_pool, block_table, seq_len, block_tokens, K_scale=No
     ptr, el = _dev_ptr, K_pool.dtype
     c = KvCache()
     c.tensors = (K_pool, V_pool, K_scale, V_scale, act_pool, block_table, seq_len)
-    c.device = K_pool.device
-    _one_device(c.device, *c.tensors)
+    c.device, c.index = K_pool.device, K_pool.get_device()
+    for t in c.tensors:
+        if t is not None and t.device != c.device:
+            raise ValueError("tensors on different devices: %s and %s" % (c.device, t.device))
     c.pool_dtype, c.B, (_, c.n_kv_heads, _, c.head_dim) = el, block_table.shape[0], K_pool.shape
     c.d_act = None if act_pool is None else act_pool.shape[2]
     P_act = 0 if act_pool is None else act_pool.shape[0]
@@ -632,12 +634,6 @@ def make_kv_cache(K_pool, V_pool, block_table, seq_len, block_tokens, K_scale=No
     c.ref = ctypes.byref(c.struct)
     c.shapes = {}
     return c
-
-
-def _one_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError("tensors on different devices: %s and %s" % (device, t.device))
 
 
 def _kv_shape(cache, n_heads, el, scale=0.0, splits=0, ln_eps=1e-5):
@@ -654,34 +650,46 @@ def _kv_shape(cache, n_heads, el, scale=0.0, splits=0, ln_eps=1e-5):
     return ref
 
 
-class _on:
-    """The device of the tensors as the current one for a call, and the stream's handle: ``stream``, or the device's current
-    stream.  What the call allocates inside belongs to that stream."""
+def _kv_ptr(t, name, dtype, size, index):
+    """Address of a contiguous tensor of that type and size on GPU `index` (None stays None).  One look at each property: these
+    calls are as short as their checks."""
+    if t is None:
+        return None
+    if t.shape != size:
+        raise ValueError("%s must be %s" % (name, list(size)))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if not t.is_cuda:
+        raise TypeError("%s must be a GPU tensor (there is no CPU path)" % name)
+    if t.get_device() != index:
+        raise ValueError("%s is on %s, the cache on cuda:%d" % (name, t.device, index))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
-    __slots__ = ("device", "stream", "guards")
 
-    def __init__(self, device, stream):
-        self.device, self.stream, self.guards = device, stream, ()
+_kv_raw = None                                               # (current device, a device's current stream) once torch is needed
 
-    def __enter__(self):
+
+def _kv_on(cache, stream, call):
+    """call(handle) with the cache's device as the current one and the handle of `stream`, or of that device's current stream.
+    What the call allocates belongs to that stream."""
+    global _kv_raw
+    if stream is None:
+        if _kv_raw is None:
+            import torch
+            _kv_raw = (torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None) or
+                       (lambda index: torch.cuda.current_stream(index).cuda_stream))
+        if _kv_raw[0]() == cache.index:
+            return call(_kv_raw[1](cache.index))
         import torch
-        if self.stream is not None:
-            if self.stream.device != self.device:
-                raise ValueError("the stream is on %s, the tensors are on %s" % (self.stream.device, self.device))
-            guard = torch.cuda.stream(self.stream)             # sets the device, too
-            guard.__enter__()
-            self.guards = (guard,)
-            return self.stream.cuda_stream
-        if torch.cuda.current_device() != self.device.index:
-            guard = torch.cuda.device(self.device)
-            guard.__enter__()
-            self.guards = (guard,)
-        return _stream_ptr(None)
-
-    def __exit__(self, *exc):
-        for guard in self.guards:
-            guard.__exit__(*exc)
-        return False
+        with torch.cuda.device(cache.index):
+            return call(_kv_raw[1](cache.index))
+    import torch
+    if stream.device != cache.device:
+        raise ValueError("the stream is on %s, the cache on %s" % (stream.device, cache.device))
+    with torch.cuda.stream(stream):                          # sets the device, too
+        return call(stream.cuda_stream)
 
 
 def kv_store(cache, k, v, x=None, n_new=None, pick=None, stream=None):
@@ -689,20 +697,15 @@ def kv_store(cache, k, v, x=None, n_new=None, pick=None, stream=None):
     T) of the ``seq_len[b]`` tokens of each request, quantised where the pools hold 8 bits.  ``pick[B, T]`` int32: the row of
     each new token (the accepted path of a tree).  ``x[B, T, d]``: layer inputs, stored where the block is an ACT block."""
     import torch
-    B, T = k.shape[:2]
-    if k.shape != v.shape or k.dim() != 4 or B != cache.B or k.shape[2:] != (cache.n_kv_heads, cache.head_dim):
-        raise ValueError("k, v: [B, T, n_kv_heads, dh] of the cache")
-    if x is not None and x.shape != (B, T, cache.n_kv_heads * cache.head_dim):
-        raise ValueError("x: [B, T, d]")
-    if n_new is not None and n_new.shape != (B,) or pick is not None and pick.shape != (B, T):
-        raise ValueError("n_new: [B], pick: [B, T]")
-    el = k.dtype
-    shape = _kv_shape(cache, cache.n_kv_heads, el)
-    _one_device(cache.device, k, v, x, n_new, pick)
-    args = (_dev_ptr(k, "k", el), _dev_ptr(v, "v", el), _dev_ptr(x, "x", el), B, T, _dev_ptr(n_new, "n_new", torch.int32),
-            _dev_ptr(pick, "pick", torch.int32))
-    with _on(cache.device, stream) as handle:
-        st = lib().hk_kv_store(shape, *args, cache.ref, handle)
+    if k.dim() != 4:
+        raise ValueError("k, v: [B, T, n_kv_heads, dh]")
+    B, T, H, i32, at = cache.B, k.shape[1], cache.n_kv_heads, torch.int32, cache.index
+    size, el = (B, T, H, cache.head_dim), k.dtype
+    shape = cache.shapes.get((H, el, 0.0, 0, 1e-5)) or _kv_shape(cache, H, el)
+    args = (shape, _kv_ptr(k, "k", el, size, at), _kv_ptr(v, "v", el, size, at),
+            _kv_ptr(x, "x", el, (B, T, H * cache.head_dim), at), B, T, _kv_ptr(n_new, "n_new", i32, (B,), at),
+            _kv_ptr(pick, "pick", i32, (B, T), at), cache.ref)
+    st = _kv_on(cache, stream, lambda handle: lib().hk_kv_store(*args, handle))
     if st != HK_OK:
         raise HybridKVError(st, "hk_kv_store")
 
@@ -714,16 +717,20 @@ def kv_load(cache, L_cap, tok_off=0, dtype=None, K_out=None, V_out=None, stream=
     import torch
     if dtype is None:
         dtype = K_out.dtype if K_out is not None else cache.pool_dtype if cache.struct.format == HK_KV_16 else torch.float16
-    size = (cache.B, cache.n_kv_heads, L_cap, cache.head_dim)
-    if (K_out is None) != (V_out is None) or K_out is not None and (tuple(K_out.shape) != size or tuple(V_out.shape) != size):
-        raise ValueError("K_out, V_out: [B, n_kv_heads, L_cap, dh]")
-    shape = _kv_shape(cache, cache.n_kv_heads, dtype)
-    _one_device(cache.device, K_out, V_out)
-    with _on(cache.device, stream) as handle:
+    B, H, at = cache.B, cache.n_kv_heads, cache.index
+    size = (B, H, L_cap, cache.head_dim)
+    shape = cache.shapes.get((H, dtype, 0.0, 0, 1e-5)) or _kv_shape(cache, H, dtype)
+    if (K_out is None) != (V_out is None):
+        raise ValueError("K_out and V_out are given together")
+
+    def call(handle):
+        nonlocal K_out, V_out
         if K_out is None:
             K_out, V_out = (torch.zeros(size, dtype=dtype, device=cache.device) for _ in range(2))
-        st = lib().hk_kv_load(shape, _dev_ptr(K_out, "K_out", dtype), _dev_ptr(V_out, "V_out", dtype), cache.B, tok_off, L_cap,
-                              cache.ref, handle)
+        return lib().hk_kv_load(shape, _kv_ptr(K_out, "K_out", dtype, size, at), _kv_ptr(V_out, "V_out", dtype, size, at), B,
+                                tok_off, L_cap, cache.ref, handle)
+
+    st = _kv_on(cache, stream, call)
     if st != HK_OK:
         raise HybridKVError(st, "hk_kv_load")
     return K_out, V_out
@@ -735,31 +742,34 @@ def kv_attn_workspace_bytes(q, cache, attn_splits=0) -> int:
     return int(lib().hk_kv_attn_workspace_bytes(_kv_shape(cache, H, q.dtype, 0.0, attn_splits), cache.B, T, cache.ref))
 
 
-def _kv_attend(entry, where, q, rows, tail, cache, T, H, layer_params, out, workspace, softmax_scale, attn_splits, stream,
-               ln_eps):
-    import torch
-    el = q.dtype
-    if q.shape[0] != cache.B or q.shape[-1] != cache.head_dim:
-        raise ValueError("q: [B, H, dh] or [B, T, H, dh] of the cache's B and dh")
-    if out is not None and out.shape != q.shape:
-        raise ValueError("out: the shape of q")
-    shape = _kv_shape(cache, H, el, softmax_scale, attn_splits, ln_eps)
-    lp = None
+def _kv_attend(where, q, size, rows, tail, cache, layer_params, out, workspace, softmax_scale, attn_splits, stream, ln_eps):
+    """The two attention calls; rows and tail: their arguments in front of and behind B."""
+    H, dh, el, at = size[-2], size[-1], q.dtype, cache.index
+    shape = cache.shapes.get((H, el, softmax_scale, attn_splits, ln_eps)) or _kv_shape(cache, H, el, softmax_scale, attn_splits, ln_eps)
+    q_ptr, lp = _kv_ptr(q, "q", el, size, at), None
     if layer_params is not None:
-        if cache.d_act is not None and cache.d_act != H * cache.head_dim or layer_params[0].shape[0] != H * cache.head_dim:
+        if cache.d_act is not None and cache.d_act != H * dh or layer_params[0].shape[0] != H * dh:
             raise ValueError("act_pool and the layer: d = H * dh")
+        for t in layer_params:
+            if t is not None and t.device != cache.device:
+                raise ValueError("the layer is on %s, the cache on %s" % (t.device, cache.device))
         lp = ctypes.byref(_params(*layer_params, el=el))
-        _one_device(cache.device, *layer_params)
     elif cache.struct.n_act_used > 0:
         raise ValueError("a cache with ACT blocks in use needs layer_params")
-    _one_device(cache.device, q, out, workspace)
-    with _on(cache.device, stream) as handle:
+    if workspace is not None and workspace.device != cache.device:
+        raise ValueError("the workspace is on %s, the cache on %s" % (workspace.device, cache.device))
+
+    def call(handle):
+        nonlocal out, workspace
         if out is None:
-            out = torch.empty_like(q) if T is None else torch.zeros_like(q)
+            import torch
+            out = torch.zeros_like(q)
         if workspace is None:
             workspace = new_workspace(kv_attn_workspace_bytes(q, cache, attn_splits), cache.device)
-        st = entry(shape, _dev_ptr(q, "q", el), *rows, cache.B, *tail, cache.ref, lp, _dev_ptr(out, "out", el),
-                   _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), handle)
+        return getattr(lib(), where)(shape, q_ptr, *rows, cache.B, *tail, cache.ref, lp, _kv_ptr(out, "out", el, size, at),
+                                     _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), handle)
+
+    st = _kv_on(cache, stream, call)
     if st != HK_OK:
         raise HybridKVError(st, where)
     return out
@@ -771,7 +781,7 @@ def kv_decode_attn(q, cache, layer_params=None, out=None, workspace=None, softma
     ``out[B, H, dh]``.  H is a multiple of the cache's n_kv_heads.  ``layer_params`` as everywhere, for ACT blocks."""
     if q.dim() != 3:
         raise ValueError("q: [B, H, dh]")
-    return _kv_attend(lib().hk_kv_decode_attn, "hk_kv_decode_attn", q, (), (), cache, None, q.shape[1], layer_params, out, workspace,
+    return _kv_attend("hk_kv_decode_attn", q, (cache.B, q.shape[1], cache.head_dim), (), (), cache, layer_params, out, workspace,
                       softmax_scale, attn_splits, stream, ln_eps)
 
 
@@ -784,18 +794,14 @@ def kv_tree_attn(q, k, v, cache, mask=None, n_nodes=None, layer_params=None, out
     import torch
     if q.dim() != 4:
         raise ValueError("q: [B, T, H, dh]")
-    B, T, H, dh = q.shape
-    size = (B, T, cache.n_kv_heads, cache.head_dim)
-    if tuple(k.shape) != size or tuple(v.shape) != size:
-        raise ValueError("k, v: [B, T, n_kv_heads, dh]")
-    if mask is not None and tuple(mask.shape) not in ((B, T), (T,)) or n_nodes is not None and tuple(n_nodes.shape) != (B,):
-        raise ValueError("mask: [B, T] or [T], n_nodes: [B]")
-    _one_device(cache.device, k, v, mask, n_nodes)
-    rows = (_dev_ptr(k, "k", q.dtype), _dev_ptr(v, "v", q.dtype))
-    tail = (T, _dev_ptr(mask, "mask", torch.int64), T if mask is not None and mask.dim() == 2 else 0,
-            _dev_ptr(n_nodes, "n_nodes", torch.int32))
-    return _kv_attend(lib().hk_kv_tree_attn, "hk_kv_tree_attn", q, rows, tail, cache, T, H, layer_params, out, workspace, softmax_scale,
-                      attn_splits, stream, ln_eps)
+    (_, T, H, _), B, dh, el, at = q.shape, cache.B, cache.head_dim, q.dtype, cache.index
+    size = (B, T, cache.n_kv_heads, dh)
+    per_request = mask is not None and mask.dim() == 2
+    rows = (_kv_ptr(k, "k", el, size, at), _kv_ptr(v, "v", el, size, at))
+    tail = (T, _kv_ptr(mask, "mask", torch.int64, (B, T) if per_request else (T,), at), T if per_request else 0,
+            _kv_ptr(n_nodes, "n_nodes", torch.int32, (B,), at))
+    return _kv_attend("hk_kv_tree_attn", q, (B, T, H, dh), rows, tail, cache, layer_params, out, workspace, softmax_scale, attn_splits,
+                      stream, ln_eps)
 
 
 def tree_mask(parents):

@@ -66,14 +66,17 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
     for (int e = 0; e < E; ++e) dst[e] = (elem_t)(o[e] / l);
 }
 
-// Joins the parts of a unit that more than one range of kv_attn_rows.h holds: the workgroup of the range in which the unit's
-// second part lies.  A wavefront takes rows in turn, DH / 64 elements a lane.
+// Joins the parts of a unit that more than one range of kv_attn_rows.h holds: kMergeRows rows of the unit whose second part
+// lies in range w.  A row is DH / 4 lanes, four elements each; a thread has all of its rows on their way.
+constexpr int kMergeRows = 32, kMergeThreads = 256;
+
 template <int DH, int DT>
-__global__ __launch_bounds__(256) void kv_rows_merge_kernel(Params p, int held)
+__global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, int held)
 {
     typedef typename Elem<DT>::T elem_t;
-    constexpr int E = DH / 64;
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wg = blockIdx.x + 1;
+    typedef elem_t vec4_t __attribute__((ext_vector_type(4)));
+    constexpr int LPR = DH / 4, RPB = kMergeThreads / LPR, kDeep = kMergeRows / RPB;
+    const int lane = threadIdx.x & 63, parts = held / kMergeRows, wg = blockIdx.x / parts + 1, part = blockIdx.x % parts;
     const int64_t total = line_total(p, lane, held);
     const int used = ranges_used(total, p.groups);
     if (wg >= used) return;
@@ -85,28 +88,49 @@ __global__ __launch_bounds__(256) void kv_rows_merge_kernel(Params p, int held)
     const int64_t first = begin + (int64_t)unit * rq.tiles;
     if (first == pos || ranges::range_begin(wg - 1, total, used) > first) return;   // the unit begins here, or its second part came before
     const int last = ranges::owner(first + rq.tiles - 1, total, used);
-    const int h = unit / rq.groups, row0 = unit % rq.groups * held;
-    const int rows = rq.nodes * p.g - row0 < held ? rq.nodes * p.g - row0 : held;
+    const int h = unit / rq.groups, row0 = unit % rq.groups * held + part * kMergeRows, rows = rq.nodes * p.g;
+    if (row0 >= rows) return;
     const float *ml = p.partial + p.slots * DH;
-    for (int i = wave; i < rows; i += 4) {
-        // the first part is that of range wg - 1, which begins the unit; the others do not
-        float m = -INFINITY, l = 0.f, o[E] = {};
-        for (int x = wg - 1; x <= last; ++x) {
-            const int64_t slot = (int64_t)(2 * x + (x == wg - 1)) * held + i;
-            const float2 v = *reinterpret_cast<const float2 *>(ml + 2 * slot);
-            const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
-            const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(v.x - ref);
-            const float *src = p.partial + slot * DH + lane * E;
-            l = l * a + v.y * b;
+    const int c = threadIdx.x % LPR, mine = threadIdx.x / LPR;
+    float m[kDeep], l[kDeep];
+    float4_t o[kDeep];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * a + src[e] * b;
-            m = top;
+    for (int u = 0; u < kDeep; ++u) {
+        m[u] = -INFINITY;
+        l[u] = 0.f;
+        o[u] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // the first part is that of range wg - 1, which begins the unit; the others do not
+    for (int x = wg - 1; x <= last; ++x) {
+        const int64_t slot0 = (int64_t)(2 * x + (x == wg - 1)) * held + part * kMergeRows + mine;
+        float2 v[kDeep];
+        float4_t s[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            const int64_t slot = slot0 + (row0 + mine + u * RPB < rows ? u * RPB : -mine);      // a row that exists
+            v[u] = *reinterpret_cast<const float2 *>(ml + 2 * slot);
+            s[u] = *reinterpret_cast<const float4_t *>(p.partial + slot * DH + 4 * c);
         }
-        const int row = row0 + i, node = row / p.g;
-        const bool some = rq.len > 0 || seen_by(p, r, node, rq.nodes) != 0;
-        elem_t *dst = static_cast<elem_t *>(p.out) + (((int64_t)r * p.T + node) * p.H + h * p.g + row % p.g) * DH + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; ++e) dst[e] = some ? (elem_t)(o[e] / l) : (elem_t)0.f;
+        for (int u = 0; u < kDeep; ++u) {
+            const float top = fmaxf(m[u], v[u].x), ref = top == -INFINITY ? 0.f : top;
+            const float a = __builtin_amdgcn_exp2f(m[u] - ref), b = __builtin_amdgcn_exp2f(v[u].x - ref);
+            l[u] = l[u] * a + v[u].y * b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * a + s[u][e] * b;
+            m[u] = top;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u) {
+        const int row = row0 + mine + u * RPB, node = row / p.g;
+        if (row >= rows) continue;
+        const bool some = rq.len > 0 || seen_by(p, r, node, rq.nodes) != 0;
+        vec4_t out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = some ? (elem_t)(o[u][e] / l[u]) : (elem_t)0.f;
+        elem_t *dst = static_cast<elem_t *>(p.out) + (((int64_t)r * p.T + node) * p.H + h * p.g + row % p.g) * DH + 4 * c;
+        *reinterpret_cast<vec4_t *>(dst) = out;
     }
 }
 
@@ -114,7 +138,8 @@ template <int DH, int DT>
 hipError_t launch_merge(const Params &p, const Plan &pl, hipStream_t s)
 {
     if (pl.shared) {
-        hipLaunchKernelGGL((kv_rows_merge_kernel<DH, DT>), dim3((unsigned)(pl.groups - 1)), dim3(256), 0, s, p, 16 * kWaves * pl.tiles);
+        const int held = 16 * kWaves * pl.tiles;
+        hipLaunchKernelGGL((kv_rows_merge_kernel<DH, DT>), dim3((unsigned)((pl.groups - 1) * (held / kMergeRows))), dim3(kMergeThreads), 0, s, p, held);
     } else {
         const int64_t rows = (int64_t)p.B * p.c.Hkv * pl.rows;
         hipLaunchKernelGGL((kv_merge_kernel<DH, DT>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);

@@ -199,28 +199,56 @@ class _Handle(hk.KvCache):
 
     def __init__(self, B=2, Hkv=2, dh=64, form=hk.HK_KV_INT8, el=torch.int8, n_act_used=0):
         self.struct = hk.hk_kv_cache(n_kv_heads=Hkv, format=form, block_tokens=16, max_blocks=4, n_act_used=n_act_used)
-        self.ref, self.tensors, self.device, self.pool_dtype = ctypes.byref(self.struct), (), torch.device("cpu"), el
+        self.ref, self.tensors, self.device, self.index, self.pool_dtype = ctypes.byref(self.struct), (), torch.device("cuda:0"), 0, el
         self.B, self.n_kv_heads, self.head_dim, self.d_act, self.shapes = B, Hkv, dh, None, {}
 
 
+class _Gpu:
+    """What the binding looks at of a GPU tensor."""
+
+    def __init__(self, *shape, dtype=torch.float16, device=0, contiguous=True, is_cuda=True):
+        self.shape, self.dtype, self.is_cuda, self._contiguous = torch.Size(shape), dtype, is_cuda, contiguous
+        self.device = torch.device("cuda:%d" % device)
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return self.device.index
+
+    def is_contiguous(self):
+        return self._contiguous
+
+    def data_ptr(self):
+        return FAKE
+
+
 def test_calls_of_the_binding_refuse_what_does_not_fit():
-    c, h = _Handle(), torch.float16
-    z = lambda *s, dtype=h: torch.zeros(*s, dtype=dtype)
-    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    c, z = _Handle(), _Gpu
+    i32 = lambda *s: _Gpu(*s, dtype=torch.int32)
     rows, q = z(2, 3, 2, 64), z(2, 3, 4, 64)
-    for bad in (lambda: hk.kv_store(c, rows, rows[:1]), lambda: hk.kv_store(c, z(2, 3, 1, 64), z(2, 3, 1, 64)),
+    class side:
+        device = torch.device("cuda:1")
+    for bad in (lambda: hk.kv_store(c, rows, z(1, 3, 2, 64)), lambda: hk.kv_store(c, z(2, 3, 1, 64), z(2, 3, 1, 64)),
                 lambda: hk.kv_store(c, z(1, 3, 2, 64), z(1, 3, 2, 64)), lambda: hk.kv_store(c, rows, rows, n_new=i32(3)),
                 lambda: hk.kv_store(c, rows, rows, pick=i32(2, 2)), lambda: hk.kv_store(c, rows, rows, x=z(2, 3, 64)),
-                lambda: hk.kv_load(c, 5, K_out=z(2, 2, 5, 64)), lambda: hk.kv_load(c, 5, K_out=z(2, 2, 4, 64), V_out=z(2, 2, 5, 64)),
+                lambda: hk.kv_store(c, z(2, 2, 64), z(2, 2, 64)), lambda: hk.kv_store(c, rows, z(2, 3, 2, 64, device=1)),
+                lambda: hk.kv_store(c, rows, rows, stream=side), lambda: hk.kv_store(c, rows, z(2, 3, 2, 64, contiguous=False)),
+                lambda: hk.kv_load(c, 5, K_out=z(2, 2, 5, 64)), lambda: hk.kv_load(c, 5, K_out=z(2, 2, 5, 64), V_out=z(2, 2, 5, 64), stream=side),
                 lambda: hk.kv_decode_attn(q, c), lambda: hk.kv_decode_attn(z(3, 4, 64), c), lambda: hk.kv_decode_attn(z(2, 4, 128), c),
-                lambda: hk.kv_decode_attn(z(2, 4, 64), c, out=z(2, 2, 64)), lambda: hk.kv_decode_attn(z(2, 2, 64), _Handle(n_act_used=1)),
-                lambda: hk.kv_tree_attn(z(2, 4, 64), rows, rows, c), lambda: hk.kv_tree_attn(q, rows[:, :2], rows, c),
-                lambda: hk.kv_tree_attn(q, rows, rows, c, mask=torch.zeros(2, dtype=torch.int64)),
-                lambda: hk.kv_tree_attn(q, rows, rows, c, n_nodes=i32(3))):
+                lambda: hk.kv_decode_attn(z(2, 4, 64, device=1), c), lambda: hk.kv_decode_attn(z(2, 2, 64), _Handle(n_act_used=1)),
+                lambda: hk.kv_decode_attn(z(2, 4, 64), c, workspace=z(4096, dtype=torch.uint8, device=1)),
+                lambda: hk.kv_decode_attn(z(2, 4, 64), c, layer_params=(z(100),) * 4),
+                lambda: hk.kv_decode_attn(z(2, 4, 64), c, layer_params=(z(256, device=1),) * 4),
+                lambda: hk.kv_tree_attn(z(2, 4, 64), rows, rows, c), lambda: hk.kv_tree_attn(q, z(2, 2, 2, 64), rows, c),
+                lambda: hk.kv_tree_attn(q, rows, z(2, 3, 4, 64), c), lambda: hk.kv_tree_attn(q, rows, rows, c, mask=z(2, dtype=torch.int64)),
+                lambda: hk.kv_tree_attn(q, rows, rows, c, mask=z(3, 3, dtype=torch.int64)), lambda: hk.kv_tree_attn(q, rows, rows, c, n_nodes=i32(3))):
         with pytest.raises(ValueError):
             bad()
-    for bad in (lambda: hk.kv_decode_attn(z(2, 4, 64, dtype=torch.float32), c), lambda: hk.kv_store(c, rows.float(), rows.float()),
-                lambda: hk.kv_decode_attn(z(2, 4, 64, dtype=torch.bfloat16), _Handle(form=hk.HK_KV_16, el=h)),
-                lambda: hk.kv_load(c, 4, dtype=torch.float32)):
+    for bad in (lambda: hk.kv_decode_attn(z(2, 4, 64, dtype=torch.float32), c), lambda: hk.kv_store(c, z(2, 3, 2, 64, dtype=torch.float32), rows),
+                lambda: hk.kv_decode_attn(z(2, 4, 64, dtype=torch.bfloat16), _Handle(form=hk.HK_KV_16, el=torch.float16)),
+                lambda: hk.kv_store(c, rows, z(2, 3, 2, 64, dtype=torch.bfloat16)), lambda: hk.kv_store(c, rows, rows, n_new=z(2, dtype=torch.int64)),
+                lambda: hk.kv_tree_attn(q, rows, rows, c, mask=i32(3)), lambda: hk.kv_store(c, rows, z(2, 3, 2, 64, is_cuda=False)),
+                lambda: hk.kv_load(c, 4, dtype=torch.float32), lambda: hk.kv_store(c, torch.zeros(2, 3, 2, 64).half(), rows)):
         with pytest.raises(TypeError):
             bad()
