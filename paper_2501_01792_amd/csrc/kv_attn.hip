@@ -20,10 +20,8 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
     const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (id >= (int64_t)p.B * p.c.Hkv * R) return;
     const int row = uniform((int)(id % R)), h = uniform((int)(id / R % p.c.Hkv)), r = uniform((int)(id / R / p.c.Hkv));
-    const int64_t C = piece_length(p, lane);
-    int n;
-    const int x0 = first_piece(p, C, r, lane, n);
-    const int nodes = nodes_of(p, r);
+    const int2 note = piece_notes(p, DH)[r];
+    const int nodes = nodes_of(p, r), x0 = uniform(note.x), n = uniform(note.y);
     if (n == 1 || row >= nodes * p.g) return;              // its only piece has written it, or there is none
     const int64_t slot0 = ((int64_t)x0 * p.c.Hkv + h) * R + row, step = (int64_t)p.c.Hkv * R;
     const float *ml = p.partial + p.slots * DH;
@@ -76,19 +74,11 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
     typedef typename Elem<DT>::T elem_t;
     typedef elem_t vec4_t __attribute__((ext_vector_type(4)));
     constexpr int LPR = DH / 4, RPB = kMergeThreads / LPR, kDeep = kMergeRows / RPB;
-    const int lane = threadIdx.x & 63, parts = held / kMergeRows, wg = blockIdx.x / parts + 1, part = blockIdx.x % parts;
-    const int64_t total = line_total(p, lane, held);
-    const int used = ranges_used(total, p.groups);
-    if (wg >= used) return;
-    const int64_t pos = ranges::range_begin(wg, total, used);
-    int64_t begin;
-    const int r = request_at(p, pos, lane, held, begin);
-    const Request rq = request(p, r, held);
-    const int unit = (int)ranges::quot(pos - begin, rq.tiles);
-    const int64_t first = begin + (int64_t)unit * rq.tiles;
-    if (first == pos || ranges::range_begin(wg - 1, total, used) > first) return;   // the unit begins here, or its second part came before
-    const int last = ranges::owner(first + rq.tiles - 1, total, used);
-    const int h = unit / rq.groups, row0 = unit % rq.groups * held + part * kMergeRows, rows = rq.nodes * p.g;
+    const int parts = held / kMergeRows, wg = blockIdx.x / parts + 1, part = blockIdx.x % parts;
+    const int4 note = reinterpret_cast<const int4 *>(p.partial + p.slots * (DH + 2))[wg];
+    const int r = uniform(note.x), h = uniform(note.y), row0 = uniform(note.z) + part * kMergeRows, n_parts = uniform(note.w);
+    if (n_parts == 0) return;                              // no unit whose second part begins this range
+    const int len = length_of(p.c, r), nodes = nodes_of(p, r), rows = nodes * p.g;
     if (row0 >= rows) return;
     const float *ml = p.partial + p.slots * DH;
     const int c = threadIdx.x % LPR, mine = threadIdx.x / LPR;
@@ -101,7 +91,7 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
         o[u] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
     // the first part is that of range wg - 1, which begins the unit; the others do not
-    for (int x = wg - 1; x <= last; ++x) {
+    for (int x = wg - 1; x < wg - 1 + n_parts; ++x) {
         const int64_t slot0 = (int64_t)(2 * x + (x == wg - 1)) * held + part * kMergeRows + mine;
         float2 v[kDeep];
         float4_t s[kDeep];
@@ -125,7 +115,7 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
     for (int u = 0; u < kDeep; ++u) {
         const int row = row0 + mine + u * RPB, node = row / p.g;
         if (row >= rows) continue;
-        const bool some = rq.len > 0 || seen_by(p, r, node, rq.nodes) != 0;
+        const bool some = len > 0 || seen_by(p, r, node, nodes) != 0;
         vec4_t out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = some ? (elem_t)(o[u][e] / l[u]) : (elem_t)0.f;

@@ -36,7 +36,7 @@ struct Params {
     const int64_t *mask;
     const int32_t *n_nodes;
     void *out;
-    float *partial;                                        // [slots, DH] sums, then [slots] (m, l)
+    float *partial;                                        // [slots, DH] sums, [slots] (m, l), what the merge has to know
     int64_t slots;
     int B, T, H, mask_stride, g, extra, groups;            // groups: workgroups of the launch
     float scale_log2e;
@@ -49,6 +49,15 @@ hipError_t launch_e4m3(const Params &p, const Plan &pl, int head_dim, int dtype,
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// Element i (wavefront-uniform) of an array that no kernel of the call writes, by a scalar load: counted apart from the loads
+// of K and V, so that waiting for it waits for nothing else.
+__device__ __forceinline__ int scalar_at(const int32_t *a, int64_t i)
+{
+    typedef const __attribute__((address_space(4))) int32_t *const_ptr_t;
+    return ((const_ptr_t)(uintptr_t)a)[i];
+}
+
+// r may differ from lane to lane.
 __device__ __forceinline__ int length_of(const KvCacheView &c, int r)
 {
     const int64_t room = (int64_t)c.max_blocks << c.blk_log2;
@@ -90,16 +99,6 @@ __device__ __forceinline__ bool locate(const Params &p, int64_t C, int x, int la
     return false;
 }
 
-// First piece of request r, and how many it has.
-__device__ __forceinline__ int first_piece(const Params &p, int64_t C, int r, int lane, int &n)
-{
-    int before = 0;
-    for (int i = lane; i < r; i += 64) before += pieces_of(length_of(p.c, i), C);
-    for (int off = 32; off > 0; off >>= 1) before += __shfl_xor(before, off, 64);
-    n = pieces_of(length_of(p.c, r), C);
-    return before;
-}
-
 __device__ __forceinline__ int nodes_of(const Params &p, int r)
 {
     const int n = p.n_nodes ? p.n_nodes[r] : p.T;
@@ -117,7 +116,7 @@ __device__ __forceinline__ uint64_t seen_by(const Params &p, int r, int i, int n
 // What a workgroup works on.
 struct Place {
     int h, x;                                              // K/V head, piece of the line of all pieces
-    int r, pieces, nodes, len, t_begin, t_end;             // request, its pieces, nodes, tokens; the piece's (the part's) tokens
+    int r, piece, pieces, nodes, len, t_begin, t_end;      // request, its pieces, nodes, tokens; the piece's (the part's) tokens
     bool last;                                             // the request's last piece, which takes the nodes, too
 };
 // false: there is nothing to do.
@@ -126,19 +125,27 @@ __device__ __forceinline__ bool place(const Params &p, int lane, Place &a)
     const int xh = blockIdx.x;
     a.h = xh % p.c.Hkv;
     a.x = xh / p.c.Hkv;
-    const int64_t C = piece_length(p, lane);
-    int r = a.x, piece = 0, pieces = 1;
-    if (p.extra > 0 && !locate(p, C, a.x, lane, r, piece, pieces)) return false;
-    a.r = uniform(r);
-    piece = uniform(piece);
-    a.pieces = uniform(pieces);
+    a.r = a.x;
+    a.piece = 0;
+    a.pieces = 1;
+    int64_t C = 0;
+    if (p.extra > 0) {
+        C = piece_length(p, lane);
+        int r, piece, pieces;
+        if (!locate(p, C, a.x, lane, r, piece, pieces)) return false;
+        a.r = uniform(r);
+        a.piece = uniform(piece);
+        a.pieces = uniform(pieces);
+    }
     a.nodes = uniform(nodes_of(p, a.r));
     a.len = uniform(length_of(p.c, a.r));
-    a.t_begin = uniform(piece == 0 ? 0 : (int)(piece * C));
-    a.last = piece + 1 == a.pieces;
+    a.t_begin = uniform((int)(a.piece * C));
+    a.last = a.piece + 1 == a.pieces;
     a.t_end = uniform(a.last ? a.len : (int)(a.t_begin + C));
     return true;
 }
+// First piece of a request and how many it has, for the merge.
+__device__ __forceinline__ int2 *piece_notes(const Params &p, int DH) { return reinterpret_cast<int2 *>(p.partial + p.slots * (DH + 2)); }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void *base, uint32_t bytes)
 {
@@ -146,17 +153,27 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void *base, uint
     const uint64_t lo = (uint32_t)uniform((int)(uint32_t)at), hi = (uint32_t)uniform((int)(uint32_t)(at >> 32));
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(hi << 32 | lo), 0, uniform((int)bytes), 0x00020000);
 }
-// N bytes (4, 8, 16) at `off`.
+// N bytes (4, 8, 16) at `off`.  Whole vectors, so that what a loop carries stays in the registers that the load fills.
 template <int N>
-struct Words {
-    uint32_t w[N / 4];
-};
+struct WordsOf;
+template <>
+struct WordsOf<4> { typedef uint32_t type; };
+template <>
+struct WordsOf<8> { typedef u32x2_t type; };
+template <>
+struct WordsOf<16> { typedef u32x4_t type; };
 template <int N>
+using Words = typename WordsOf<N>::type;
+__device__ __forceinline__ uint32_t word(uint32_t v, int) { return v; }
+__device__ __forceinline__ uint32_t word(u32x2_t v, int i) { return v[i]; }
+__device__ __forceinline__ uint32_t word(u32x4_t v, int i) { return v[i]; }
+constexpr int kStreamed = 2;                               // cache policy of rows that one workgroup reads: non-temporal
+template <int N, int AUX = 0>
 __device__ __forceinline__ Words<N> fetch(__amdgpu_buffer_rsrc_t rs, int off)
 {
-    if constexpr (N == 16) return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
-    else if constexpr (N == 8) return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
-    else return __builtin_bit_cast(Words<N>, __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0));
+    if constexpr (N == 16) return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, AUX));
+    else if constexpr (N == 8) return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, AUX));
+    else return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, AUX);
 }
 
 // The largest over the four lane groups of a row.
@@ -170,6 +187,27 @@ __device__ __forceinline__ float max_over_groups(float v)
     a = s[0];
     b = s[1];
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+// The scales of a tile, one a lane (`sc`: K's in lanes 0 .. 31, V's in the others), as its scores and weights take them: [0, 32)
+// K's times the softmax scale, [32, 64) log2 of V's, [96, 128) the reciprocals of V's.  Tokens that do not exist (n0, n1 of the two
+// 16s do): 0 s - inf, and no part of the denominator.
+constexpr int kScales = 4 * kTileTokens;
+__device__ __forceinline__ const float *scale_at(const float *ks0, const float *ks1, const float *vs0, const float *vs1, int lane)
+{
+    const uintptr_t k0 = reinterpret_cast<uintptr_t>(ks0), k1 = reinterpret_cast<uintptr_t>(ks1);
+    const uintptr_t v0 = reinterpret_cast<uintptr_t>(vs0), v1 = reinterpret_cast<uintptr_t>(vs1);
+    const uintptr_t a = lane & 16 ? k1 : k0, b = lane & 16 ? v1 : v0;
+    return reinterpret_cast<const float *>(lane < 32 ? a : b) + (lane & 15);
+}
+__device__ __forceinline__ void put_scales(float *to, float sc, int n0, int n1, int lane, float scale)
+{
+    const int tok = lane & 31;
+    const bool in = (tok & 15) < (tok < 16 ? n0 : n1);
+    const float v = sc < kLeastScale ? kLeastScale : sc;
+    const float lv = in ? __builtin_amdgcn_logf(v) : -INFINITY, kq = in ? sc * scale : 0.f;
+    to[lane] = lane < 32 ? kq : lv;
+    to[64 + lane] = in ? __builtin_amdgcn_rcpf(v) : 0.f;
 }
 
 // Waits until at most N of this wavefront's loads are on their way.
@@ -193,7 +231,7 @@ struct Wave {
     static constexpr int EB = FMT == k16 ? 2 : 1, RB = DH * EB;       // bytes of an element, of a row
     static constexpr int VB = NI * EB;                     // bytes of a token that a lane reads of V
     static constexpr int KR = FMT == k16 ? KK : KK / 2;    // 16-byte pieces of a token that a lane reads of K
-    static constexpr int kTileLoads = 2 * KR + (FMT == k16 ? 0 : 4) + 8;
+    static constexpr int kTileLoads = 2 * KR + (FMT == k16 ? 0 : 1) + 8;
 
     mvec8_t qf[MT][KK];
     float qfac[MT];                                        // the power of two that a row's query was divided by
@@ -236,6 +274,7 @@ struct Wave {
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) qf[mt][kk] = *reinterpret_cast<const mvec8_t *>(qrow[mt] + k_elem(kk));
     }
+    // The queries as the products over the cache take them.
     __device__ __forceinline__ void start()
     {
 #pragma unroll
@@ -258,6 +297,12 @@ struct Wave {
                     for (int j = 0; j < 8; ++j) qf[mt][kk][j] = (_Float16)__builtin_amdgcn_ldexpf((float)raw[kk][j], -ex);
                 qfac[mt] = __builtin_amdgcn_ldexpf(1.f, ex);
             }
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
             m[mt] = -INFINITY;
             l[mt] = 0.f;
 #pragma unroll
@@ -381,21 +426,21 @@ struct Wave {
 
     // V^T of 32 tokens, of which this lane read raw[s] of token slot s: the operands of the elements in word w, two of 16 bits
     // (as they are) or four codes (as fp16).
-    template <int N>
-    static __device__ __forceinline__ void turn16(const Words<N> (&raw)[8], int w, u32x4_t (&vt)[2])
+    template <typename W>
+    static __device__ __forceinline__ void turn16(const W (&raw)[8], int w, u32x4_t (&vt)[2])
     {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) vt[i][s] = __builtin_amdgcn_perm(raw[2 * s + 1].w[w], raw[2 * s].w[w], i ? 0x07060302u : 0x05040100u);
+            for (int s = 0; s < 4; ++s) vt[i][s] = __builtin_amdgcn_perm(word(raw[2 * s + 1], w), word(raw[2 * s], w), i ? 0x07060302u : 0x05040100u);
     }
-    template <int N>
-    static __device__ __forceinline__ void turn8(const Words<N> (&raw)[8], int w, u32x4_t (&vt)[4])
+    template <typename W>
+    static __device__ __forceinline__ void turn8(const W (&raw)[8], int w, u32x4_t (&vt)[4])
     {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {                      // token slots 4 q .. 4 q + 3
-            const uint32_t a = biased<FMT>(raw[4 * q].w[w]), b = biased<FMT>(raw[4 * q + 1].w[w]);
-            const uint32_t c = biased<FMT>(raw[4 * q + 2].w[w]), d = biased<FMT>(raw[4 * q + 3].w[w]);
+            const uint32_t a = biased<FMT>(word(raw[4 * q], w)), b = biased<FMT>(word(raw[4 * q + 1], w));
+            const uint32_t c = biased<FMT>(word(raw[4 * q + 2], w)), d = biased<FMT>(word(raw[4 * q + 3], w));
             const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
             const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
             const uint32_t e[4] = {__builtin_amdgcn_perm(cd0, ab0, 0x05040100u), __builtin_amdgcn_perm(cd0, ab0, 0x07060302u),
@@ -416,7 +461,8 @@ struct Wave {
     };
     Words<16> kraw[2][KR];
     Words<VB> vraw[8];
-    float4_t ks[2], vs[2];
+    float sc;                                              // a scale (8 bits), see put_scales
+    float *scales;                                         // LDS of the wavefront
 
     __device__ __forceinline__ void ask_k(const Tokens &tk)
     {
@@ -424,26 +470,21 @@ struct Wave {
         for (int j = 0; j < 2; ++j) {
             const __amdgpu_buffer_rsrc_t rs = rows_at(tk.K[j], tk.n[j] * RB);
 #pragma unroll
-            for (int i = 0; i < KR; ++i) kraw[j][i] = fetch<16>(rs, r16 * RB + k_elem(FMT == k16 ? i : 2 * i) * EB);
+            for (int i = 0; i < KR; ++i) kraw[j][i] = fetch<16, kStreamed>(rs, r16 * RB + k_elem(FMT == k16 ? i : 2 * i) * EB);
         }
-        if constexpr (FMT != k16) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                ks[j] = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.ks[j], 64), g4 * 16));
-                vs[j] = __builtin_bit_cast(float4_t, fetch<16>(rows_at(tk.vs[j], 64), g4 * 16));
-            }
-        }
+        if constexpr (FMT != k16) sc = *scale_at(tk.ks[0], tk.ks[1], tk.vs[0], tk.vs[1], 16 * g4 + r16);
     }
     __device__ __forceinline__ void ask_v(const Tokens &tk)
     {
         const __amdgpu_buffer_rsrc_t rs[2] = {rows_at(tk.V[0], tk.n[0] * RB), rows_at(tk.V[1], tk.n[1] * RB)};
 #pragma unroll
-        for (int s = 0; s < 8; ++s) vraw[s] = fetch<VB>(rs[s >> 2], (4 * g4 + (s & 3)) * RB + r16 * VB);
+        for (int s = 0; s < 8; ++s) vraw[s] = fetch<VB, kStreamed>(rs[s >> 2], (4 * g4 + (s & 3)) * RB + r16 * VB);
     }
-    // Takes the tokens in; n as they were asked for.  `next`, when there is one, is asked for as registers fall free.
-    __device__ __forceinline__ void take(const int (&n)[2], const Tokens &next, bool more)
+    // Takes the tokens in; n as they were asked for.  `next` is asked for as registers fall free.
+    __device__ __forceinline__ void take(const int (&n)[2], const Tokens &next)
     {
-        float4_t t[MT][2];
+        float4_t t[MT][2], inv[2];
+        if constexpr (FMT != k16) put_scales(scales, sc, n[0], n[1], 16 * g4 + r16, scale);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             mvec8_t kf[KK];
@@ -454,7 +495,7 @@ struct Wave {
                 } else {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const uint32_t b = biased<FMT>(kraw[j][i].w[w]);
+                        const uint32_t b = biased<FMT>(kraw[j][i][w]);
                         const half2_t lo = pair_f16<FMT, false>(b), hi = pair_f16<FMT, true>(b);
                         mvec8_t &f = kf[2 * i + (w >> 1)];
                         const int at = 4 * (w & 1);
@@ -469,36 +510,26 @@ struct Wave {
                 for (int kk = 0; kk < KK; ++kk) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf[kk], qf[mt][kk], t[mt][j]);
             }
         }
-        // 8 bits: t = score * scale log2(e) + log2(vs), and the denominator's factor 1 / vs
-        float4_t inv[2];
-        if constexpr (FMT != k16) {
+        if constexpr (FMT != k16) {                        // t = score * scale log2(e) + log2(vs), and the denominator's factor 1 / vs
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4_t kq = *reinterpret_cast<const float4_t *>(scales + 16 * j + 4 * g4);
+                const float4_t lv = *reinterpret_cast<const float4_t *>(scales + 32 + 16 * j + 4 * g4);
+                inv[j] = *reinterpret_cast<const float4_t *>(scales + 96 + 16 * j + 4 * g4);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[mt][j][i] = __builtin_fmaf(DT != MDT ? t[mt][j][i] * qfac[mt] : t[mt][j][i], kq[i], lv[i]);
+            }
+        } else if (n[0] + n[1] < kTileTokens) {            // tokens that do not exist
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float kq = ks[j][i] * scale;
-                    const float v = vs[j][i] < kLeastScale ? kLeastScale : vs[j][i];
-                    const float lv = __builtin_amdgcn_logf(v);
-                    inv[j][i] = __builtin_amdgcn_rcpf(v);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        const float s = DT != MDT ? t[mt][j][i] * qfac[mt] : t[mt][j][i];
-                        t[mt][j][i] = __builtin_fmaf(s, kq, lv);
-                    }
-                }
+                    for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = 4 * g4 + i < n[j] ? t[mt][j][i] : -INFINITY;
         }
-        if (n[0] + n[1] < kTileTokens) {                   // tokens that do not exist
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool in = 4 * g4 + i < n[j];
-                    if constexpr (FMT != k16) inv[j][i] = in ? inv[j][i] : 0.f;
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = in ? t[mt][j][i] : -INFINITY;
-                }
-        }
-        if (more) ask_k(next);
+        ask_k(next);
         __builtin_amdgcn_sched_barrier(0);
         mvec8_t pf[MT];
         float ref[MT];
@@ -511,9 +542,12 @@ struct Wave {
             u32x4_t vt[G];
             if constexpr (FMT == k16) turn16(vraw, w, vt);
             else turn8(vraw, w, vt);
-            if (w == NI / G - 1) {                         // the last of vraw has been read
-                __builtin_amdgcn_sched_barrier(0);
-                if (more) ask_v(next);
+            if (w == NI / G - 1) {
+                // vraw has been read before it is asked for again: else the compiler keeps both, and the loop copies, that is
+                // waits for, what has just been asked for
+#pragma unroll
+                for (int i = 0; i < G; ++i) asm volatile("" : "+v"(vt[i])::"memory");
+                ask_v(next);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
@@ -528,29 +562,26 @@ struct Wave {
     __device__ __forceinline__ void drafted(const elem_t *K, const elem_t *V, int pitch, int first, int n)
     {
         const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * pitch + DH * 2 : 0;
-        float4_t t[MT][2];
-        {
-            const __amdgpu_buffer_rsrc_t rs = rows_at(K, bytes);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                vec8_t kf[KK];
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(vec8_t, fetch<16>(rs, (16 * j + r16) * pitch + (kk * 32 + g4 * 8) * 2));
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk)
-                        t[mt][j] = Elem<DT>::mfma_16x16x32(kf[kk], *reinterpret_cast<const vec8_t *>(qrow[mt] + kk * 32 + g4 * 8), t[mt][j]);
-                }
-            }
-        }
+        const __amdgpu_buffer_rsrc_t krs = rows_at(K, bytes), vrs = rows_at(V, bytes);
+        Words<16> kraw[2][KK];
         Words<NI * 2> raw[8];
-        {
-            const __amdgpu_buffer_rsrc_t rs = rows_at(V, bytes);
 #pragma unroll
-            for (int s = 0; s < 8; ++s) raw[s] = fetch<NI * 2>(rs, (16 * (s >> 2) + 4 * g4 + (s & 3)) * pitch + r16 * NI * 2);
-        }
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) kraw[j][kk] = fetch<16>(krs, (16 * j + r16) * pitch + (kk * 32 + g4 * 8) * 2);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) raw[s] = fetch<NI * 2>(vrs, (16 * (s >> 2) + 4 * g4 + (s & 3)) * pitch + r16 * NI * 2);
+        float4_t t[MT][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, kraw[j][kk]),
+                                                       *reinterpret_cast<const vec8_t *>(qrow[mt] + kk * 32 + g4 * 8), t[mt][j]);
+            }
         // A weight of zero does not take an infinity or a NaN out of the product: such elements are zeros there and reach
         // the rows that see them on their own.
         constexpr uint32_t ex = DT == 1 ? 0x7f80u : 0x7c00u;
@@ -559,7 +590,7 @@ struct Wave {
         for (int s = 0; s < 8; ++s)
 #pragma unroll
             for (int w = 0; w < NI / 2; ++w) {
-                const uint32_t x = raw[s].w[w];
+                const uint32_t x = word(raw[s], w);
                 wild |= ((x & ex) + (ex & -ex) & 0x8000u) | ((x >> 16 & ex) + (ex & -ex) & 0x8000u);   // an exponent of ones carries
             }
         const bool any_wild = __ballot(wild != 0) != 0;
@@ -568,8 +599,8 @@ struct Wave {
             for (int s = 0; s < 8; ++s)
 #pragma unroll
                 for (int w = 0; w < NI / 2; ++w) {
-                    const uint32_t x = raw[s].w[w];
-                    raw[s].w[w] = ((x & ex) == ex ? 0u : x & 0xffffu) | ((x >> 16 & ex) == ex ? 0u : x & 0xffff0000u);
+                    const uint32_t x = word(raw[s], w);
+                    raw[s][w] = ((x & ex) == ex ? 0u : x & 0xffffu) | ((x >> 16 & ex) == ex ? 0u : x & 0xffff0000u);
                     __builtin_amdgcn_sched_barrier(0);
                 }
         }
@@ -614,20 +645,24 @@ struct Wave {
     }
 };
 
-// Table entries of the two 16s of the tile at token t (the last tile's second 16 may not exist: the first's entry stands in).
+// Table entries of the two 16s of the tile at token t; 16s that do not exist: the last one's that does (t_end > 0).
 __device__ __forceinline__ void entries_of(const int32_t *__restrict__ tab, int t, int t_end, int blk_log2, int (&e)[2])
 {
-    e[0] = tab[t >> blk_log2];
-    e[1] = tab[(t + 16 < t_end ? t + 16 : t) >> blk_log2];
+    const int last = t_end - 1;
+    e[0] = scalar_at(tab, (t < last ? t : last) >> blk_log2);
+    e[1] = scalar_at(tab, (t + 16 < last ? t + 16 : last) >> blk_log2);
 }
 
+// Where the tile's rows are.  Also for a tile behind the last: it has no rows, and a load of it reads nothing (the scales: those
+// of a block that exists).  Loops ask for it like for any other; a branch around the loads would have every pass copy, and so
+// wait for, what is on its way.
 template <typename wave_t, int FMT>
 __device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_end, const int (&ent)[2], typename wave_t::Tokens &tk)
 {
     const int blk = 1 << p.c.blk_log2;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int here = t_end - (t0 + 16 * j), t = here > 0 ? t0 + 16 * j : t0;
+        const int t = t0 + 16 * j, here = t_end - t;
         tk.n[j] = here < 0 ? 0 : here < 16 ? here : 16;
         const int e = uniform(ent[j]);
         bool act = FMT == k16 && e < 0;
@@ -648,63 +683,71 @@ __device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_
 }
 
 // Wavefronts of a SIMD that the registers are held to.
-constexpr int residency(int DH, int MT) { return MT == 1 && DH == 64 ? 3 : 2; }
+constexpr int residency(int DH, int FMT, int MT) { return MT == 2 ? 2 : DH == 64 ? 4 : FMT == k16 ? 3 : 4; }
 
 template <int DH, int DT, int FMT, int MT, bool TREE>
-__global__ __launch_bounds__(kThreads, residency(DH, MT)) void kv_attn_kernel(Params p)
+__global__ __launch_bounds__(kThreads, TREE ? 2 : residency(DH, FMT, MT)) void kv_attn_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
     constexpr int NI = wave_t::NI;
     __shared__ float join_ml[kWaves][MT * 16][2];
-    __shared__ float4_t join_o[MT * NI * 64];
+    __shared__ float4_t join_o[kWaves][MT * NI * 64];
+    __shared__ __align__(16) float scales[FMT == k16 ? 1 : kWaves][FMT == k16 ? 4 : kScales];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     Place at;
+    int ent[2] = {0, 0};
+    if (p.extra <= 0 && p.c.max_blocks > 0) {
+        // The first tile's table entries, asked for together with the length that says whether they count.
+        const int32_t *tab = p.c.block_table + (int64_t)(blockIdx.x / p.c.Hkv) * p.c.max_blocks;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int b = (wave * kTileTokens + 16 * j) >> p.c.blk_log2;
+            ent[j] = scalar_at(tab, b < p.c.max_blocks ? b : p.c.max_blocks - 1);
+        }
+    }
     if (!place(p, lane, at)) return;
     constexpr int first_row = 0;
+    if (p.slots > 0 && at.piece == 0 && at.h == 0 && threadIdx.x == 0) piece_notes(p, DH)[at.r] = make_int2(at.x, at.pieces);
     if (at.nodes <= 0) return;                             // no rows
     wave_t w;
     w.rows(p, at, first_row, lane, TREE);
+    w.scales = scales[FMT == k16 ? 0 : wave];
+    w.clear();
     w.ask_q();
-    const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
-    const int t_end = at.t_end;
-    int tb = at.t_begin + wave * kTileTokens;              // pieces begin at whole rounds: wavefront 0 takes the first tile
-    typename wave_t::Tokens tk;
-    int ent[2] = {0, 0};
-    if (tb < t_end) {
-        entries_of(tab, tb, t_end, p.c.blk_log2, ent);
-        tokens_at<wave_t, FMT>(p, at.h, tb, t_end, ent, tk);
-        w.ask_k(tk);
-        w.ask_v(tk);
-        w.start();
-        if (tb + kStep < t_end) entries_of(tab, tb + kStep, t_end, p.c.blk_log2, ent);
-        // Said once, in front of the loop: the queries are there.  Else every pass would wait for all that is on its way.
-        wait_loads<wave_t::kTileLoads>();
-        do {
-            const int n[2] = {tk.n[0], tk.n[1]};
-            const bool more = tb + kStep < t_end;
-            if (more) tokens_at<wave_t, FMT>(p, at.h, tb + kStep, t_end, ent, tk);
-            if (tb + 2 * kStep < t_end) entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
-            w.take(n, tk, more);
-            tb += kStep;
-        } while (tb < t_end);
-    } else {
-        w.start();
-    }
-    if (TREE && p.k && at.last) {
-        const int turn = (t_end - at.t_begin + kTileTokens - 1) / kTileTokens;
+    if (TREE && p.k && at.last) {                          // the nodes, by the wavefronts that have the fewest tiles
         const int pitch = p.c.Hkv * DH * 2;
         for (int d = 0; d * kTileTokens < at.nodes; ++d) {
-            if ((turn + d) % kWaves != wave) continue;
+            if (kWaves - 1 - d != wave) continue;
             const int64_t from = (((int64_t)at.r * p.T + d * kTileTokens) * p.c.Hkv + at.h) * DH;
             const int n = at.nodes - d * kTileTokens;
             w.drafted(static_cast<const elem_t *>(p.k) + from, static_cast<const elem_t *>(p.v) + from, pitch, d * kTileTokens,
                       n < kTileTokens ? n : kTileTokens);
         }
     }
+    const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
+    const int t_end = at.t_end;
+    int tb = at.t_begin + wave * kTileTokens;              // pieces begin at whole rounds: wavefront 0 takes the first tile
+    if (tb < t_end) {
+        typename wave_t::Tokens tk;
+        if (p.extra > 0) entries_of(tab, tb, t_end, p.c.blk_log2, ent);
+        tokens_at<wave_t, FMT>(p, at.h, tb, t_end, ent, tk);
+        w.ask_k(tk);
+        w.ask_v(tk);
+        entries_of(tab, tb + kStep, t_end, p.c.blk_log2, ent);
+        w.start();
+        // Said once, in front of the loop: the queries are there.  Else every pass would wait for all that is on its way.
+        wait_loads<wave_t::kTileLoads>();
+        do {
+            const int n[2] = {tk.n[0], tk.n[1]};
+            tokens_at<wave_t, FMT>(p, at.h, tb + kStep, t_end, ent, tk);
+            entries_of(tab, tb + 2 * kStep, t_end, p.c.blk_log2, ent);
+            w.take(n, tk);
+            tb += kStep;
+        } while (tb < t_end);
+    }
 
-    // The wavefronts' results about their common maximum, added in the order of the wavefronts.
-    float ref[MT];
+    // The wavefronts' results about their common maximum, added in the order of the wavefronts; each stores a part of the row.
     w.sum_denominators();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -712,40 +755,53 @@ __global__ __launch_bounds__(kThreads, residency(DH, MT)) void kv_attn_kernel(Pa
             join_ml[wave][mt * 16 + w.r16][0] = w.m[mt];
             join_ml[wave][mt * 16 + w.r16][1] = w.l[mt];
         }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) join_o[wave][(mt * NI + i) * 64 + lane] = w.o[mt][i];
     }
     __syncthreads();
+    constexpr int NQ = NI / kWaves;                        // products whose results this wavefront joins
+    const int64_t slot0 = ((int64_t)at.x * p.c.Hkv + at.h) * ((int64_t)p.T * p.g);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        float top = -INFINITY;
+        const int row = mt * 16 + w.r16;
+        if (row >= at.nodes * p.g) continue;
+        float top = -INFINITY, l = 0.f, f[kWaves];
 #pragma unroll
-        for (int q = 0; q < kWaves; ++q) top = fmaxf(top, join_ml[q][mt * 16 + w.r16][0]);
-        ref[mt] = top == -INFINITY ? 0.f : top;
-        const float mine = __builtin_amdgcn_exp2f(w.m[mt] - ref[mt]);
+        for (int q = 0; q < kWaves; ++q) top = fmaxf(top, join_ml[q][row][0]);
+        const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int i = 0; i < NI; ++i) w.o[mt][i] *= mine;
-        float l = 0.f;
-#pragma unroll
-        for (int q = 0; q < kWaves; ++q) l += join_ml[q][mt * 16 + w.r16][1] * __builtin_amdgcn_exp2f(join_ml[q][mt * 16 + w.r16][0] - ref[mt]);
-        w.l[mt] = l;
-        w.m[mt] = top;
-    }
-    for (int q = 1; q < kWaves; ++q) {
-        if (wave == q) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int i = 0; i < NI; ++i) join_o[(mt * NI + i) * 64 + lane] = w.o[mt][i];
+        for (int q = 0; q < kWaves; ++q) {
+            f[q] = __builtin_amdgcn_exp2f(join_ml[q][row][0] - ref);
+            l = __builtin_fmaf(join_ml[q][row][1], f[q], l);
         }
-        __syncthreads();
-        if (wave == 0) {
+        float4_t sum[NQ];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+        for (int i = 0; i < NQ; ++i) {
+            sum[i] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < NI; ++i) w.o[mt][i] += join_o[(mt * NI + i) * 64 + lane];
+            for (int q = 0; q < kWaves; ++q) sum[i] += join_o[q][(mt * NI + wave * NQ + i) * 64 + lane] * f[q];
         }
-        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int elem = (4 * w.g4 + e) * NI + wave * NQ;
+            if (at.pieces == 1) {
+                elem_t *dst = static_cast<elem_t *>(p.out) + (w.qrow[mt] - static_cast<const elem_t *>(p.q)) + elem;
+                typedef elem_t vec_t __attribute__((ext_vector_type(NQ)));
+                vec_t v;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) v[i] = w.some >> mt & 1 ? (elem_t)(sum[i][e] / l) : (elem_t)0.f;
+                *reinterpret_cast<vec_t *>(dst) = v;
+            } else {
+                typedef float fvec_t __attribute__((ext_vector_type(NQ)));
+                fvec_t v;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) v[i] = sum[i][e];
+                *reinterpret_cast<fvec_t *>(p.partial + (slot0 + row) * DH + elem) = v;
+            }
+        }
+        if (at.pieces > 1 && wave == 0 && w.g4 == 0)
+            *reinterpret_cast<float2 *>(p.partial + p.slots * DH + 2 * (slot0 + row)) = make_float2(top, l);
     }
-    if (wave == 0) w.store(p, at, first_row, at.pieces == 1, ((int64_t)at.x * p.c.Hkv + at.h) * ((int64_t)p.T * p.g));
 }
 
 }  // namespace kvattn

@@ -24,7 +24,7 @@ template <int DH>
 struct Operands {
     u32x4_t k[2 * (DH / 32)][64];                          // [16s of tokens x products][lane]
     u32x4_t v[DH / 16][64];
-    float scales[4 * kTileTokens];                         // K's scale * softmax scale, log2 of V's, -, 1 / V's
+    float scales[kScales];                                 // see put_scales
     int wild;                                              // V of a tile of nodes holds infinities or NaN
 };
 
@@ -64,14 +64,11 @@ struct Part {
                 const __amdgpu_buffer_rsrc_t rs = rows_at(q ? r.V1 : r.V0, bytes(r, q));
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
-                    vraw[4 * half + s] = fetch<4>(rs, (4 * g4 + s) * r.pitch + r16 * VB + v_word(wave) * 4).w[0];
+                    vraw[4 * half + s] = fetch<4>(rs, (4 * g4 + s) * r.pitch + r16 * VB + v_word(wave) * 4);
             }
         }
         if constexpr (kCodes) {                            // a scale a lane: those of K in lanes 0 .. 31, of V in the others
-            const uintptr_t k0 = reinterpret_cast<uintptr_t>(r.ks0), k1 = reinterpret_cast<uintptr_t>(r.ks1);
-            const uintptr_t v0 = reinterpret_cast<uintptr_t>(r.vs0), v1 = reinterpret_cast<uintptr_t>(r.vs1);
-            const uintptr_t a = lane & 16 ? k1 : k0, b = lane & 16 ? v1 : v0;
-            sc = reinterpret_cast<const float *>(lane < 32 ? a : b)[r16];
+            sc = *scale_at(r.ks0, r.ks1, r.vs0, r.vs1, lane);
         }
     }
     static __device__ __forceinline__ uint32_t bytes(const Rows &r, int j)
@@ -94,7 +91,7 @@ struct Part {
                         u32x4_t f;
 #pragma unroll
                         for (int w = 0; w < 2; ++w) {
-                            const uint32_t b = biased<F>(kraw[i].w[2 * half + w]);
+                            const uint32_t b = biased<F>(kraw[i][2 * half + w]);
                             f[2 * w] = __builtin_bit_cast(uint32_t, pair_f16<F, false>(b));
                             f[2 * w + 1] = __builtin_bit_cast(uint32_t, pair_f16<F, true>(b));
                         }
@@ -129,14 +126,8 @@ struct Part {
             }
         }
         if constexpr (kCodes) {
-            // Every wavefront stores the same: a branch would part the products from what runs under them.  A token that does
-            // not exist: 0 s - inf, and no part of the denominator.
-            const int tok = lane & 31;
-            const bool in = (tok & 15) < (tok < 16 ? n0 : n1), of_k = lane < 32;
-            const float v = sc < kLeastScale ? kLeastScale : sc;
-            const float lv = in ? __builtin_amdgcn_logf(v) : -INFINITY, kq = in ? sc * scale : 0.f;
-            to.scales[lane] = of_k ? kq : lv;
-            to.scales[64 + lane] = in ? __builtin_amdgcn_rcpf(v) : 0.f;          // of V in the upper half
+            // every wavefront stores the same: a branch would part the products from what runs under them
+            put_scales(to.scales, sc, n0, n1, lane, scale);
         }
     }
     // Infinities and NaN of V become zeros (16-bit rows); whether there were any.
@@ -224,6 +215,7 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
     const int used = ranges_used(total, p.groups);
     // Workgroups go to the 8 XCDs in turn: neighbours on the line, which read the same rows, on one of them.
     const int b = blockIdx.x, wg = p.groups % 8 == 0 ? (b & 7) * (p.groups / 8) + (b >> 3) : b;
+    if (p.slots > 0 && threadIdx.x == 0) reinterpret_cast<int4 *>(p.partial + p.slots * (DH + 2))[wg] = int4{0, 0, 0, 0};
     if (wg >= used || total <= 0) return;
     int64_t pos = ranges::range_begin(wg, total, used);
     const int64_t end = ranges::range_begin(wg + 1, total, used);
@@ -250,21 +242,25 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
         const int node_begin = (first > of_tokens ? first - of_tokens : 0) * kTileTokens;
         const int node_end = p.k && first + n > of_tokens ? (first + n - of_tokens) * kTileTokens : 0;
         const int group_first = unit % rq.groups * kHeld, first_row = group_first + wave * MT * 16;
+        if (first > 0 && threadIdx.x == 0 && pos - first >= ranges::range_begin(wg - 1, total, used))
+            // for the merge, at the unit's second part: request, head, first row, number of parts
+            reinterpret_cast<int4 *>(p.partial + p.slots * (DH + 2))[wg] =
+                int4{at.r, at.h, group_first, ranges::owner(pos - first + rq.tiles - 1, total, used) - wg + 2};
         pos += n;
 
         wave_t w;
         w.rows(p, at, first_row, lane, true);
+        w.clear();
         w.ask_q();
         const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
         // Rows are asked for three tiles ahead (two wait in registers, in turn), their table entries four.
         Part<DH, FMT> part[2];
         int ent[2] = {0, 0}, t_ask = at.t_begin;
         auto ask = [&](Part<DH, FMT> &to) {
-            if (t_ask >= at.t_end) return;
             typename wave_t::Tokens tk;
             tokens_at<wave_t, FMT>(p, at.h, t_ask, at.t_end, ent, tk);
             t_ask += kTileTokens;
-            if (t_ask < at.t_end) entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
+            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
             Rows r = {tk.K[0], tk.K[1], tk.V[0], tk.V[1], nullptr, nullptr, nullptr, nullptr, tk.n[0], tk.n[1], wave_t::RB};
             if constexpr (FMT != k16) { r.ks0 = tk.ks[0]; r.ks1 = tk.ks[1]; r.vs0 = tk.vs[0]; r.vs1 = tk.vs[1]; }
             to.ask(r, wave, lane);

@@ -40,7 +40,7 @@ struct Plan {
     int64_t extra;           // S
     int64_t groups;          // workgroups of the launch
     int64_t slots;           // rows of unfinished results
-    int64_t partial_floats;
+    int64_t partial_floats;  // slots of head_dim sums, then of (m, l), then what the merge has to know of a request or range
 };
 
 inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int64_t total_tokens, int splits)
@@ -73,7 +73,7 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
         p.groups = (B + S) * Hkv;
         p.slots = S > 0 ? p.groups * p.rows : 0;
     }
-    p.partial_floats = p.slots * (head_dim + 2);
+    p.partial_floats = p.slots > 0 ? p.slots * (head_dim + 2) + (p.shared ? 4 * p.groups : 2 * B) : 0;
     return p;
 }
 
