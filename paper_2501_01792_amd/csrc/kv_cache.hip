@@ -21,20 +21,26 @@ __device__ __forceinline__ bool block_of(const KvCacheView &c, int r, int t, int
     return *e >= 0 ? *e < c.P_kv : ~*e < c.P_act;
 }
 
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+
 template <int FMT, int DT>
 __device__ __forceinline__ void put8(void *pool, float *scales, int64_t row, int DH, int c, u32x4_t raw)
 {
     typedef typename Elem<DT>::V8 vec8_t;
     if constexpr (FMT == k16) {
-        *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(pool) + row * DH + 8 * c) = raw;
+        __builtin_nontemporal_store(raw, reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(pool) + row * DH + 8 * c));
     } else {
-        uint32_t top = 0;
+        // the largest magnitude, two at a time, then among the row's lanes (8 or 16 neighbours: moves on the vector ALU)
+        typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+        u16x2_t two = {0, 0};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = raw[j] & 0x7fffu, hi = raw[j] >> 16 & 0x7fffu;
-            top = max(top, max(lo, hi));
-        }
-        for (int off = DH / 16; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+        for (int j = 0; j < 4; ++j) two = __builtin_elementwise_max(two, __builtin_bit_cast(u16x2_t, raw[j] & 0x7fff7fffu));
+        uint32_t top = max((uint32_t)two[0], (uint32_t)two[1]);
+        top = max(top, moved<0xb1>(top));                  // lane ^ 1
+        top = max(top, moved<0x4e>(top));                  // lane ^ 2
+        top = max(top, moved<0x141>(top));                 // lane ^ 7
+        if (DH == 128) top = max(top, moved<0x128>(top));  // lane ^ 8
         const bool finite = top < (DT == 1 ? 0x7f80u : 0x7c00u);
         const float most_x = (float)__builtin_bit_cast(typename Elem<DT>::T, (uint16_t)top);
         float scale = most_x / most<FMT>();
@@ -43,8 +49,9 @@ __device__ __forceinline__ void put8(void *pool, float *scales, int64_t row, int
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = finite ? (float)v[j] : 0.f;
-        const u32x2_t code = encode8<FMT>(x, finite ? scale : 1.f);
-        *reinterpret_cast<u32x2_t *>(static_cast<uint8_t *>(pool) + row * DH + 8 * c) = code;
+        scale = finite ? scale : 1.f;
+        const u32x2_t code = encode8<FMT>(x, scale, 1.f / scale);
+        __builtin_nontemporal_store(code, reinterpret_cast<u32x2_t *>(static_cast<uint8_t *>(pool) + row * DH + 8 * c));
         if (c == 0) scales[row] = finite ? scale : __builtin_nanf("");
     }
 }
@@ -100,7 +107,7 @@ __device__ __forceinline__ u32x4_t widen8(u32x2_t code, float scale)
     return __builtin_bit_cast(u32x4_t, v);
 }
 
-constexpr int kLoadRows = 4;                               // rows a thread has on the way
+constexpr int kLoadRows = 2;                               // rows a thread has on the way
 
 template <int DH, int DT, int FMT>
 __global__ __launch_bounds__(kThreads) void kv_load_kernel(KvLoadArgs a, int tiles)
@@ -131,8 +138,8 @@ __global__ __launch_bounds__(kThreads) void kv_load_kernel(KvLoadArgs a, int til
         for (int u = 0; u < kLoadRows; ++u)
             if (to[u] >= 0) {
                 const int64_t at = ((int64_t)pair * a.L_cap + to[u]) * DH + 8 * c;
-                *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.K_out) + at) = k[u];
-                *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.V_out) + at) = v[u];
+                __builtin_nontemporal_store(k[u], reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.K_out) + at));
+                __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.V_out) + at));
             }
     } else {
         u32x2_t k[kLoadRows], v[kLoadRows];
@@ -149,8 +156,8 @@ __global__ __launch_bounds__(kThreads) void kv_load_kernel(KvLoadArgs a, int til
         for (int u = 0; u < kLoadRows; ++u)
             if (to[u] >= 0) {
                 const int64_t at = ((int64_t)pair * a.L_cap + to[u]) * DH + 8 * c;
-                *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.K_out) + at) = widen8<FMT, DT>(k[u], ks[u]);
-                *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.V_out) + at) = widen8<FMT, DT>(v[u], vs[u]);
+                __builtin_nontemporal_store(widen8<FMT, DT>(k[u], ks[u]), reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.K_out) + at));
+                __builtin_nontemporal_store(widen8<FMT, DT>(v[u], vs[u]), reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(a.V_out) + at));
             }
     }
 }

@@ -23,24 +23,31 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 template <int FMT>
 __device__ __forceinline__ constexpr float most() { return FMT == kInt8 ? 127.f : 448.f; }
 
-// 8 elements of a row -> 8 codes.  scale is finite and not below kLeastScale.
+// 8 elements of a row -> 8 codes.  scale is finite and not below kLeastScale, inv = 1 / scale (rounded correctly, as the
+// language's division is).  x / scale rounded correctly comes from two multiply-adds on x inv, its residue times inv added on: the
+// last steps of a division, without the scaling that keeps a general one out of the ranges that cannot occur here.
 template <int FMT>
-__device__ __forceinline__ u32x2_t encode8(const float (&x)[8], float scale)
+__device__ __forceinline__ u32x2_t encode8(const float (&x)[8], float scale, float inv)
 {
     u32x2_t code;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        if constexpr (FMT == kInt8) {
-            uint32_t v = 0;
+        float y[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float y = __builtin_rintf(x[4 * w + j] / scale);          // |y| <= 127 up to the quotient's rounding
-                v |= ((uint32_t)(int)fminf(fmaxf(y, -127.f), 127.f) & 0xffu) << (8 * j);
-            }
-            code[w] = v;
+        for (int j = 0; j < 4; ++j) {
+            const float q = x[4 * w + j] * inv;
+            y[j] = __builtin_fmaf(__builtin_fmaf(-q, scale, x[4 * w + j]), inv, q);
+        }
+        if constexpr (FMT == kInt8) {
+            // |y| <= 127 up to the quotient's rounding; at 1.5 * 2^23 a float's last bit is one, so the sum rounds to nearest
+            // even and its low byte is the code
+            uint32_t b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(uint32_t, y[j] + 12582912.f);
+            code[w] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
         } else {
-            int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w] / scale, x[4 * w + 1] / scale, 0, false);
-            code[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2] / scale, x[4 * w + 3] / scale, v, true);
+            const int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            code[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
         }
     }
     return code;
