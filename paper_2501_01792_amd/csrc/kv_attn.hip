@@ -79,38 +79,47 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
     const int r = uniform(note.x), h = uniform(note.y), row0 = uniform(note.z) + part * kMergeRows, n_parts = uniform(note.w);
     if (n_parts == 0) return;                              // no unit whose second part begins this range
     const int len = length_of(p.c, r), nodes = nodes_of(p, r), rows = nodes * p.g;
-    if (row0 >= rows) return;
     const float *ml = p.partial + p.slots * DH;
     const int c = threadIdx.x % LPR, mine = threadIdx.x / LPR;
+    // the first part is that of range wg - 1, which begins the unit; the others do not
+    auto slot_of = [&](int x) { return (int64_t)(2 * x + (x == wg - 1)) * held + part * kMergeRows + mine; };
+    float2 v[2][kDeep];
+    float4_t s[2][kDeep];
+    auto ask = [&](int x, int b) {                         // also rows that there are not: what their slots hold is not used
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            v[b][u] = *reinterpret_cast<const float2 *>(ml + 2 * (slot_of(x) + u * RPB));
+            s[b][u] = *reinterpret_cast<const float4_t *>(p.partial + (slot_of(x) + u * RPB) * DH + 4 * c);
+        }
+    };
     float m[kDeep], l[kDeep];
     float4_t o[kDeep];
+    auto add = [&](int b) {
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            const float top = fmaxf(m[u], v[b][u].x), ref = top == -INFINITY ? 0.f : top;
+            const float f = __builtin_amdgcn_exp2f(m[u] - ref), g = __builtin_amdgcn_exp2f(v[b][u].x - ref);
+            l[u] = l[u] * f + v[b][u].y * g;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * f + s[b][u][e] * g;
+            m[u] = top;
+        }
+    };
+    ask(wg - 1, 0);                                        // two parts at least: both on their way at once
+    ask(wg, 1);
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
         m[u] = -INFINITY;
         l[u] = 0.f;
         o[u] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
-    // the first part is that of range wg - 1, which begins the unit; the others do not
-    for (int x = wg - 1; x < wg - 1 + n_parts; ++x) {
-        const int64_t slot0 = (int64_t)(2 * x + (x == wg - 1)) * held + part * kMergeRows + mine;
-        float2 v[kDeep];
-        float4_t s[kDeep];
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-            const int64_t slot = slot0 + (row0 + mine + u * RPB < rows ? u * RPB : -mine);      // a row that exists
-            v[u] = *reinterpret_cast<const float2 *>(ml + 2 * slot);
-            s[u] = *reinterpret_cast<const float4_t *>(p.partial + slot * DH + 4 * c);
-        }
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-            const float top = fmaxf(m[u], v[u].x), ref = top == -INFINITY ? 0.f : top;
-            const float a = __builtin_amdgcn_exp2f(m[u] - ref), b = __builtin_amdgcn_exp2f(v[u].x - ref);
-            l[u] = l[u] * a + v[u].y * b;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * a + s[u][e] * b;
-            m[u] = top;
-        }
+    add(0);
+    add(1);
+    for (int x = wg + 1; x < wg - 1 + n_parts; ++x) {
+        ask(x, 0);
+        add(0);
     }
+    if (row0 >= rows) return;
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
         const int row = row0 + mine + u * RPB, node = row / p.g;

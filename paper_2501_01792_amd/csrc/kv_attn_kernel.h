@@ -228,6 +228,7 @@ struct Wave {
     static constexpr int MDT = FMT == k16 ? DT : 0;        // type of the products over the cache
     typedef typename Elem<MDT>::V8 mvec8_t;
     static constexpr int KK = DH / 32, NI = DH / 16;
+    static constexpr bool kOwnQ = DT == MDT;               // the products over the nodes take the same queries
     static constexpr int EB = FMT == k16 ? 2 : 1, RB = DH * EB;       // bytes of an element, of a row
     static constexpr int VB = NI * EB;                     // bytes of a token that a lane reads of V
     static constexpr int KR = FMT == k16 ? KK : KK / 2;    // 16-byte pieces of a token that a lane reads of K
@@ -264,6 +265,14 @@ struct Wave {
             seen[mt] = tree ? seen_by(p, at.r, node, at.nodes) : 0;
             some |= (at.len > 0 || seen[mt] != 0) << mt;
         }
+    }
+
+    // The same for the products over the nodes, and the query's operand there.
+    __device__ __forceinline__ int node_elem(int kk) const { return kOwnQ ? k_elem(kk) : kk * 32 + g4 * 8; }
+    __device__ __forceinline__ vec8_t node_query(int mt, int kk) const
+    {
+        if constexpr (kOwnQ) return __builtin_bit_cast(vec8_t, qf[mt][kk]);
+        else return *reinterpret_cast<const vec8_t *>(qrow[mt] + node_elem(kk));
     }
 
     // The queries are asked for before the first rows of K and V: a wait for the latter is then one for the former, too.
@@ -568,7 +577,7 @@ struct Wave {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) kraw[j][kk] = fetch<16>(krs, (16 * j + r16) * pitch + (kk * 32 + g4 * 8) * 2);
+            for (int kk = 0; kk < KK; ++kk) kraw[j][kk] = fetch<16>(krs, (16 * j + r16) * pitch + node_elem(kk) * 2);
 #pragma unroll
         for (int s = 0; s < 8; ++s) raw[s] = fetch<NI * 2>(vrs, (16 * (s >> 2) + 4 * g4 + (s & 3)) * pitch + r16 * NI * 2);
         float4_t t[MT][2];
@@ -579,8 +588,7 @@ struct Wave {
                 t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk)
-                    t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, kraw[j][kk]),
-                                                       *reinterpret_cast<const vec8_t *>(qrow[mt] + kk * 32 + g4 * 8), t[mt][j]);
+                    t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, kraw[j][kk]), node_query(mt, kk), t[mt][j]);
             }
         // A weight of zero does not take an infinity or a NaN out of the product: such elements are zeros there and reach
         // the rows that see them on their own.

@@ -10,6 +10,8 @@
 #pragma once
 #include "kv_attn_kernel.h"
 
+#include <type_traits>
+
 namespace hk {
 namespace kvattn {
 
@@ -48,6 +50,8 @@ struct Part {
     static __device__ __forceinline__ int v_word(int wave) { return kSplit ? 0 : NV == 8 ? wave : wave & 1; }
     static __device__ __forceinline__ int v_quad(int wave) { return kSplit ? wave & 1 : NV == 8 ? 0 : wave >> 1; }
 
+    // codes_order: 16-bit rows whose products take queries that are laid out for codes.
+    template <bool codes_order = kCodes>
     __device__ __forceinline__ void ask(const Rows &r, int wave, int lane)
     {
         const int g4 = lane >> 4, r16 = lane & 15;
@@ -55,7 +59,10 @@ struct Part {
             const int j = k_sixteen(wave);
             const __amdgpu_buffer_rsrc_t rs = rows_at(j ? r.K1 : r.K0, bytes(r, j));
 #pragma unroll
-            for (int i = 0; i < NK; ++i) kraw[i] = fetch<16>(rs, r16 * r.pitch + k_piece(wave, i) * 64 + g4 * 16);
+            for (int i = 0; i < NK; ++i) {
+                const int kk = k_piece(wave, i);
+                kraw[i] = fetch<16>(rs, r16 * r.pitch + (codes_order && !kCodes ? (kk >> 1) * 128 + g4 * 32 + (kk & 1) * 16 : kk * 64 + g4 * 16));
+            }
         }
         if (!kSplit || wave >= 2) {
 #pragma unroll
@@ -255,12 +262,11 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
         const int32_t *tab = p.c.block_table + (int64_t)at.r * p.c.max_blocks;
         // Rows are asked for three tiles ahead (two wait in registers, in turn), their table entries four.
         Part<DH, FMT> part[2];
-        int ent[2] = {0, 0}, t_ask = at.t_begin;
-        auto ask = [&](Part<DH, FMT> &to) {
+        int ent[2], t_ask = at.t_begin;
+        auto ask = [&](Part<DH, FMT> &to, const int (&e)[2]) {
             typename wave_t::Tokens tk;
-            tokens_at<wave_t, FMT>(p, at.h, t_ask, at.t_end, ent, tk);
+            tokens_at<wave_t, FMT>(p, at.h, t_ask, at.t_end, e, tk);
             t_ask += kTileTokens;
-            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
             Rows r = {tk.K[0], tk.K[1], tk.V[0], tk.V[1], nullptr, nullptr, nullptr, nullptr, tk.n[0], tk.n[1], wave_t::RB};
             if constexpr (FMT != k16) { r.ks0 = tk.ks[0]; r.ks1 = tk.ks[1]; r.vs0 = tk.vs[0]; r.vs1 = tk.vs[1]; }
             to.ask(r, wave, lane);
@@ -269,125 +275,151 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
             const int here = at.t_end - t;
             from.put(to, here < 16 ? here : 16, here < 16 ? 0 : here < 32 ? here - 16 : 16, wave, lane, w.scale);
         };
-        // One tile: its successor's operands are made from `next`, which then waits for the tile two behind that.
-        auto tile = [&](int tb, const Operands<DH> &op, Operands<DH> &op_next, Part<DH, FMT> &next) {
-            // Operands are asked of LDS well ahead: K's before the next tile's are made, V's before the weights.
-            mvec8_t kf[2 * KK], vf[NI];
-            float4_t kq[2], lv[2], inv[2];
+        // One tile: its successor's operands are made from `next`, which then waits for the tile two behind that.  A wavefront
+        // whose rows do not exist only makes operands.
+        const bool mine = first_row < at.nodes * p.g;
+        auto tile = [&](auto has_rows, int tb, const Operands<DH> &op, Operands<DH> &op_next, Part<DH, FMT> &next) {
+            if constexpr (!decltype(has_rows)::value) {
+                put(next, tb + kTileTokens, op_next);
+            } else {
+                // Operands are asked of LDS well ahead: K's before the next tile's are made, V's before the weights.
+                mvec8_t kf[2 * KK], vf[NI];
+                float4_t kq[2], lv[2], inv[2];
 #pragma unroll
-            for (int i = 0; i < 2 * KK; ++i) kf[i] = __builtin_bit_cast(mvec8_t, op.k[i][lane]);
-            if constexpr (FMT != k16) {
+                for (int i = 0; i < 2 * KK; ++i) kf[i] = __builtin_bit_cast(mvec8_t, op.k[i][lane]);
+                if constexpr (FMT != k16) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    kq[j] = *reinterpret_cast<const float4_t *>(op.scales + 16 * j + 4 * w.g4);
-                    lv[j] = *reinterpret_cast<const float4_t *>(op.scales + 32 + 16 * j + 4 * w.g4);
-                    inv[j] = *reinterpret_cast<const float4_t *>(op.scales + 96 + 16 * j + 4 * w.g4);
+                    for (int j = 0; j < 2; ++j) {
+                        kq[j] = *reinterpret_cast<const float4_t *>(op.scales + 16 * j + 4 * w.g4);
+                        lv[j] = *reinterpret_cast<const float4_t *>(op.scales + 32 + 16 * j + 4 * w.g4);
+                        inv[j] = *reinterpret_cast<const float4_t *>(op.scales + 96 + 16 * j + 4 * w.g4);
+                    }
                 }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            put(next, tb + kTileTokens, op_next);              // behind the last tile: what nobody reads
-            float4_t t[MT][2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
+                __builtin_amdgcn_sched_barrier(0);
+                put(next, tb + kTileTokens, op_next);              // behind the last tile: what nobody reads
+                float4_t t[MT][2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf[j * KK + kk], w.qf[mt][kk], t[mt][j]);
+                    for (int mt = 0; mt < MT; ++mt) t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < NI; ++i) vf[i] = __builtin_bit_cast(mvec8_t, op.v[i][lane]);
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (FMT != k16) {
+                for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                        for (int mt = 0; mt < MT; ++mt) t[mt][j] = Elem<MDT>::mfma_16x16x32(kf[j * KK + kk], w.qf[mt][kk], t[mt][j]);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) vf[i] = __builtin_bit_cast(mvec8_t, op.v[i][lane]);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (FMT != k16) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                t[mt][j][i] = __builtin_fmaf(DT != MDT ? t[mt][j][i] * w.qfac[mt] : t[mt][j][i], kq[j][i], lv[j][i]);
+                } else if (at.t_end - tb < kTileTokens) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            t[mt][j][i] = __builtin_fmaf(DT != MDT ? t[mt][j][i] * w.qfac[mt] : t[mt][j][i], kq[j][i], lv[j][i]);
-            } else if (at.t_end - tb < kTileTokens) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                            for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = tb + 16 * j + 4 * w.g4 + i < at.t_end ? t[mt][j][i] : -INFINITY;
+                }
+                mvec8_t pf[MT];
+                float ref[MT];
+                w.references(t, ref);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                for (int mt = 0; mt < MT; ++mt) {                  // one tile's products run under the next one's weights
+                    w.weigh(mt, t[mt], inv, ref[mt], pf[mt]);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) t[mt][j][i] = tb + 16 * j + 4 * w.g4 + i < at.t_end ? t[mt][j][i] : -INFINITY;
+                    for (int i = 0; i < NI; ++i) w.o[mt][i] = Elem<MDT>::mfma_16x16x32(vf[i], pf[mt], w.o[mt][i]);
+                }
             }
-            mvec8_t pf[MT];
-            float ref[MT];
-            w.references(t, ref);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {                  // one tile's products run under the next one's weights
-                w.weigh(mt, t[mt], inv, ref[mt], pf[mt]);
-#pragma unroll
-                for (int i = 0; i < NI; ++i) w.o[mt][i] = Elem<MDT>::mfma_16x16x32(vf[i], pf[mt], w.o[mt][i]);
-            }
-            ask(next);
+            ask(next, ent);
+            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
             meet();                                            // the next tile is there, and this one's buffer is free
         };
         if (at.t_begin < at.t_end) {
-            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
-            ask(part[0]);
-            ask(part[1]);
+            int ent0[2], ent1[2];
+            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent0);
+            entries_of(tab, t_ask + kTileTokens, at.t_end, p.c.blk_log2, ent1);
+            entries_of(tab, t_ask + 2 * kTileTokens, at.t_end, p.c.blk_log2, ent);
+            ask(part[0], ent0);
+            ask(part[1], ent1);
             w.start();
             put(part[0], at.t_begin, ops[0]);
             // Said once, in front of the loop: the queries are there.  Else every tile would wait for all that is on its way.
             wait_loads<Part<DH, FMT>::kLoads>();
-            ask(part[0]);
+            ask(part[0], ent);
+            entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
             meet();
-            int tb = at.t_begin;
-            do {
-                tile(tb, ops[0], ops[1], part[1]);
-                if (tb + kTileTokens < at.t_end) tile(tb + kTileTokens, ops[1], ops[0], part[0]);
-                tb += 2 * kTileTokens;
-            } while (tb < at.t_end);
+            auto tiles = [&](auto has_rows) {
+                int tb = at.t_begin;
+                do {
+                    tile(has_rows, tb, ops[0], ops[1], part[1]);
+                    if (tb + kTileTokens < at.t_end) tile(has_rows, tb + kTileTokens, ops[1], ops[0], part[0]);
+                    tb += 2 * kTileTokens;
+                } while (tb < at.t_end);
+            };
+            if (mine) tiles(std::true_type());
+            else tiles(std::false_type());
         } else {
             w.start();
         }
 
-        const int pitch = p.c.Hkv * DH * 2;
-        for (int node = node_begin; node < node_end && node < at.nodes; node += kTileTokens) {
-            const int64_t from = (((int64_t)at.r * p.T + node) * p.c.Hkv + at.h) * DH;
-            const elem_t *K = static_cast<const elem_t *>(p.k) + from, *V = static_cast<const elem_t *>(p.v) + from;
-            const int here = at.nodes - node < kTileTokens ? at.nodes - node : kTileTokens;
-            const Rows r = {K, reinterpret_cast<const char *>(K) + 16 * pitch, V, reinterpret_cast<const char *>(V) + 16 * pitch,
-                            nullptr, nullptr, nullptr, nullptr, here < 16 ? here : 16, here < 16 ? 0 : here - 16, pitch};
-            Part<DH, k16> nodes;
-            nodes.ask(r, wave, lane);
-            if (threadIdx.x == 0) ops[0].wild = 0;
+        if (node_begin < node_end && node_begin < at.nodes) {
+            // the nodes' tiles, two at most, both asked for at once
+            const int pitch = p.c.Hkv * DH * 2;
+            Part<DH, k16> nodes[2];
+            Rows r[2];
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                const int node = node_begin + d * kTileTokens, upto = at.nodes < node_end ? at.nodes : node_end;
+                const int64_t from = (((int64_t)at.r * p.T + node) * p.c.Hkv + at.h) * DH;
+                const elem_t *K = static_cast<const elem_t *>(p.k) + from, *V = static_cast<const elem_t *>(p.v) + from;
+                const int here = upto - node;
+                r[d] = {K, reinterpret_cast<const char *>(K) + 16 * pitch, V, reinterpret_cast<const char *>(V) + 16 * pitch,
+                        nullptr, nullptr, nullptr, nullptr, here < 0 ? 0 : here < 16 ? here : 16,
+                        here < 16 ? 0 : here < 32 ? here - 16 : 16, pitch};
+                nodes[d].template ask<FMT != k16 && wave_t::kOwnQ>(r[d], wave, lane);
+            }
+            if (threadIdx.x < 2) ops[threadIdx.x].wild = 0;
             meet();
-            if (nodes.template tame<DT>() && lane == 0) ops[0].wild = 1;
-            nodes.put(ops[0], r.n0, r.n1, wave, lane, 0.f);
-            meet();
-            const Operands<DH> &op = ops[0];
-            float4_t t[MT][2];
-            vec8_t pf[MT];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int d = 0; d < 2; ++d) {
+                if (r[d].n0 <= 0) break;
+                if (nodes[d].template tame<DT>() && lane == 0) ops[d].wild = 1;
+                nodes[d].put(ops[d], r[d].n0, r[d].n1, wave, lane, 0.f);
+                meet();
+                const Operands<DH> &op = ops[d];
+                float4_t t[MT][2];
+                vec8_t pf[MT];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int kk = 0; kk < KK; ++kk)
-                        t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, op.k[j * KK + kk][lane]),
-                                                           *reinterpret_cast<const vec8_t *>(w.qrow[mt] + kk * 32 + w.g4 * 8), t[mt][j]);
+                    for (int j = 0; j < 2; ++j) {
+                        t[mt][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int kk = 0; kk < KK; ++kk)
+                            t[mt][j] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, op.k[j * KK + kk][lane]), w.node_query(mt, kk), t[mt][j]);
+                    }
+                const int node = node_begin + d * kTileTokens;
+                w.weigh_nodes(t, node, pf);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const vec8_t vf = __builtin_bit_cast(vec8_t, op.v[i][lane]);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) w.o[mt][i] = Elem<DT>::mfma_16x16x32(vf, pf[mt], w.o[mt][i]);
+                }
+                if (uniform(op.wild)) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        w.add_wild(static_cast<const elem_t *>(r[d].V0), pitch, node, r[d].n0 + r[d].n1, mt, t[mt]);
                 }
             }
-            w.weigh_nodes(t, node, pf);
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const vec8_t vf = __builtin_bit_cast(vec8_t, op.v[i][lane]);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) w.o[mt][i] = Elem<DT>::mfma_16x16x32(vf, pf[mt], w.o[mt][i]);
-            }
-            if (uniform(op.wild)) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) w.add_wild(V, pitch, node, here, mt, t[mt]);
-            }
-            meet();
+            meet();                                        // the operands have been read: the range's next unit may store its own
         }
         w.sum_denominators();
         // a range has one part that does not begin its unit at most, and one that begins a unit and does not end it

@@ -26,7 +26,8 @@ constexpr int kTileTokens = 32;                      // tokens a wavefront takes
 constexpr int kWaves = 4;
 constexpr int kStep = kTileTokens * kWaves;          // tokens of a round of a workgroup whose wavefronts share them out
 constexpr int kMaxTiles = 2;                         // tiles of 16 query rows in a wavefront
-constexpr int kWantGroups = 1024;                    // workgroups that fill the chip: 256 compute units x 4
+constexpr int kWantGroups = 1024;                    // workgroups that fill the chip: 256 compute units x 4 (two tiles: x 2)
+constexpr int kWholeTokens = 512;                    // requests that short on average are not cut: the merge is a launch of its own
 constexpr int kLeastRange = 4;                       // tiles of a range at least
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
@@ -62,10 +63,11 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
     } else {
         p.tiles = (int)all;
         int64_t S = 0;
+        const int64_t want = kWantGroups / p.tiles;
         if (splits > 0) {
             S = splits > 1 ? B * splits : 0;
-        } else if (B * Hkv < kWantGroups) {
-            S = (kWantGroups + Hkv - 1) / Hkv - B;
+        } else if (B * Hkv < want && total_tokens > kWholeTokens * B) {
+            S = (want + Hkv - 1) / Hkv - B;
             const int64_t most = total_tokens / kStep;       // a piece has a round at least
             S = S < most ? S : most;
         }

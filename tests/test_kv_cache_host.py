@@ -128,7 +128,7 @@ def test_refusals_of_the_attention_calls():
     assert _decode(q=FAKE + 2) == hk.HK_ERR_ALIGN and _decode(ws=FAKE + 16) == hk.HK_ERR_ALIGN
     assert _decode(hk.make_shape(4096, 31)) == hk.HK_ERR_SHAPE and _decode(hk.make_shape(4096, 32, dtype=2)) == hk.HK_ERR_DTYPE
     assert _decode(B=-1) == hk.HK_ERR_SHAPE and _decode(B=(1 << 20) + 1, total_tokens=0) == hk.HK_ERR_SHAPE
-    assert _decode(ws_bytes=64, total_tokens=512) == hk.HK_ERR_WORKSPACE
+    assert _decode(ws_bytes=64, max_blocks=4096, total_tokens=100000) == hk.HK_ERR_WORKSPACE
     assert _decode(P_kv=0) == hk.HK_ERR_SHAPE                                            # tokens but no block to hold them
     assert _decode(B=0, total_tokens=0) == hk.HK_OK
     # checkpoints: 16 bits, a K/V head of its own for every query head, and the layer
