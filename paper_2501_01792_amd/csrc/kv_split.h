@@ -32,7 +32,7 @@ constexpr int kLeastRange = 4;                       // tiles of a range at leas
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
 // Workgroups of a compute unit that the registers of the shared form leave room for.
-HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 ? (tiles == 1 ? 4 : 3) : tiles == 1 ? 3 : 2; }
+HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 && tiles == 1 ? 3 : 2; }
 
 struct Plan {
     int64_t rows;            // T * g
