@@ -624,9 +624,32 @@ struct Wave {
                 for (int i = 0; i < 2; ++i)
                     o[mt][2 * w + i] = Elem<DT>::mfma_16x16x32(__builtin_bit_cast(vec8_t, vt[i]), pf[mt], o[mt][2 * w + i]);
         }
+        if constexpr (FMT != k16) lift();
         if (any_wild) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) add_wild(V, pitch, first, n, mt, t[mt]);
+        }
+    }
+    // The nodes came first, and the rows of the cache, whose scores hold log2 of their scales of V, may all lie far below the
+    // nodes' maximum where V is small: their weights would be below fp16's numbers.  So the maximum goes down as far as the sums
+    // have room for; rows of the cache that still lie below it are less than 2^-90 of the sums.
+    __device__ __forceinline__ void lift()
+    {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float top = l[mt];
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, __builtin_fabsf(o[mt][i][e]));
+            top = max_over_groups(top);
+            const int ex = top > 0.f ? __builtin_amdgcn_frexp_expf(top) : 100, up = ex < 100 ? 100 - ex : 0;
+            m[mt] -= (float)up;
+            l[mt] = __builtin_amdgcn_ldexpf(l[mt], up);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[mt][i][e] = __builtin_amdgcn_ldexpf(o[mt][i][e], up);
         }
     }
     // The infinities and NaN of V, node by node; t: the weights of this lane's row and tokens.

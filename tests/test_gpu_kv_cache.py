@@ -260,6 +260,43 @@ def test_scales_of_every_size(form, dtype):
     check_attention("scales", c, q[:, None], None, None, None, None, out[:, None])
 
 
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,power", [("f16", -12), ("f16", 10), ("bf16", -40), ("bf16", 40)])
+@pytest.mark.parametrize("T", [5, 30])
+def test_a_tree_keeps_the_bits_of_small_and_large_v(form, dtype, power, T):
+    """V of cache and nodes far from one: the nodes' rows have no scale that stands beside the tokens' ones."""
+    lens, H, Hkv, dh, bt = [300, 70, 0], 4, 2, 64, 16
+    c = Cache(100, form, dtype, lens, Hkv, dh, bt)
+    q, k, v = normal(101, 3, T, H, dh, dtype=dtype), normal(102, 3, T, Hkv, dh, dtype=dtype), normal(103, 3, T, Hkv, dh, dtype=dtype)
+    for splits in (0, 3):
+        c.scales[1].mul_(2.0 ** power)
+        out = hk.kv_tree_attn(q, k, v * 2.0 ** power, c.handle, attn_splits=splits)
+        if dtype == "bf16":                                # exact powers of two: held to the tolerance at V of size one
+            c.scales[1].mul_(2.0 ** -power)
+            check_attention("power", c, q, k, v, None, None, out.double() * 2.0 ** -power)
+        else:
+            check_attention("power", c, q, k, v * 2.0 ** power, None, None, out)
+            c.scales[1].mul_(2.0 ** -power)
+
+
+def test_many_short_requests_and_one_long_one():
+    """More requests than a wavefront has lanes, most of them short or empty, in every form that cuts their tokens."""
+    rng = np.random.default_rng(104)
+    lens = [int(n) for n in rng.integers(0, 40, 150)]
+    lens[3], lens[64], lens[130], lens[149] = 0, 5000, 0, 700
+    for form, T, H in (("int8", 1, 8), ("16", 3, 8), ("e4m3", 9, 16), ("int8", 17, 40)):
+        c = Cache(105, form, "f16", lens, 2, 64, 32)
+        q, k, v = normal(106, 150, T, H, 64), normal(107, 150, T, 2, 64), normal(108, 150, T, 2, 64)
+        nodes = rng.integers(0, T + 1, 150).astype(np.int32)
+        for splits in (0, 1, 2):
+            if T == 1:
+                check_attention("ragged", c, q, None, None, None, None, hk.kv_decode_attn(q[:, 0].contiguous(), c.handle, attn_splits=splits)[:, None])
+            else:
+                out = torch.full_like(q, 7.0)
+                hk.kv_tree_attn(q, k, v, c.handle, n_nodes=torch.from_numpy(nodes).cuda(), out=out, attn_splits=splits)
+                check_attention("ragged", c, q, k, v, None, nodes, out, untouched=7.0)
+
+
 # ------------------------------------------------------------------ trees
 def random_masks(seed, B, T, kind):
     rng = np.random.default_rng(seed)
