@@ -1149,7 +1149,7 @@ int hk_kv_load(const hk_shape *shape, void *K_out, void *V_out, int32_t B, int32
     int st = kv_view(shape, B, cache, &a.c);
     if (st != HK_OK) return st;
     if (tok_off < 0 || L_cap < 0 || tok_off > (1 << 30) || L_cap > (1 << 30)) return HK_ERR_SHAPE;
-    if ((int64_t)B * cache->n_kv_heads * (((int64_t)L_cap + 63) / 64) > (1 << 23)) return HK_ERR_SHAPE;
+    if ((int64_t)B * cache->n_kv_heads * (((int64_t)L_cap + 31) / 32) > (1 << 23)) return HK_ERR_SHAPE;    // workgroups of a launch
     if (B == 0 || L_cap == 0) return HK_OK;
     st = kv_pointers(cache);
     if (st != HK_OK) return st;

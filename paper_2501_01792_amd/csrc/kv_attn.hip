@@ -156,6 +156,8 @@ size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, in
 bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits)
 {
     const kvattn::Plan pl = kvattn::plan(B, T, H, Hkv, head_dim, total_tokens, splits);
+    // the launches of both forms and of their merges
+    if (pl.shared) return pl.groups * (16 * kvattn::kWaves * pl.tiles / kvattn::kMergeRows) <= kvattn::kMostGroups;
     return pl.groups <= kvattn::kMostGroups && B * Hkv * pl.rows <= 4 * kvattn::kMostGroups;
 }
 

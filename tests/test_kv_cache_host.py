@@ -152,6 +152,8 @@ def test_refusals_of_store_and_load():
     assert _store(T=0) == hk.HK_OK and _store(B=0, total_tokens=0) == hk.HK_OK
     assert _load(K=None) == hk.HK_ERR_NULL and _load(V=None) == hk.HK_ERR_NULL and _load(K=FAKE + 8) == hk.HK_ERR_ALIGN
     assert _load(off=-1) == hk.HK_ERR_SHAPE and _load(L=-1) == hk.HK_ERR_SHAPE and _load(L=1 << 30) == hk.HK_ERR_SHAPE
+    # a launch holds fewer than 2^32 threads: 4 requests x 8 heads x 2^18 workgroups of 32 tokens are the last that fit
+    assert _load(K=None, L=1 << 23) == hk.HK_ERR_NULL and _load(K=None, L=(1 << 23) + 1) == hk.HK_ERR_SHAPE
     assert _load(L=0) == hk.HK_OK and _load(B=0, total_tokens=0) == hk.HK_OK
 
 
@@ -164,6 +166,15 @@ def test_workspace_is_known_before_the_pools_are():
     assert ask(1, 8, **big) >= ask(1, 1, **big) > 256
     hybrid = dict(format=hk.HK_KV_16, P_act=64, n_act_used=64, n_kv_heads=32)
     assert ask(4, 1, **hybrid) >= 2 * 64 * 16 * 4096 * 2
+
+
+def test_cuts_that_no_launch_holds_are_refused():
+    """At most 2^23 workgroups of 256: the pieces of 8 K/V heads (one row), or 2^21 ranges that are merged by 4 (512 rows)."""
+    size = hk.lib().hk_kv_attn_workspace_bytes
+    shape = hk.make_shape(4096, 32, attn_splits=64)
+    ask = lambda B, T: size(ctypes.byref(shape), B, T, ctypes.byref(_cache(max_blocks=1 << 13, total_tokens=B << 17)))
+    assert ask(16131, 1) > 0 and ask(16132, 1) == 0        # 16131 * 65 * 8 <= 2^23
+    assert ask(1 << 12, 64) > 0 and ask((1 << 12) + 1, 64) == 0
 
 
 def test_struct_layout():
