@@ -1063,7 +1063,9 @@ int make_kv_attn_plan(const hk_shape *s, int64_t B, int64_t T, const hk_kv_cache
     if (c->total_tokens > 0 && c->P_kv == 0 && c->n_act_used == 0) return HK_ERR_SHAPE;      // tokens but no block to hold them
     p->view.P_act = c->n_act_used;
     if (c->P_kv == 0 && c->n_act_used == 0) p->view.max_blocks = 0;                          // whatever the lengths say
-    if (!hk::kv_attn_launchable(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, c->total_tokens, s->attn_splits)) return HK_ERR_SHAPE;
+    const bool codes = c->format != HK_KV_16;
+    const int64_t room = (int64_t)p->view.max_blocks * c->block_tokens;
+    if (!hk::kv_attn_launchable(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, codes, c->total_tokens, room, s->attn_splits)) return HK_ERR_SHAPE;
     p->M = (int64_t)c->n_act_used * c->block_tokens;
     if (p->M > 0x7fffffffLL) return HK_ERR_SHAPE;
     p->scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / std::sqrt((float)s->head_dim);
@@ -1074,7 +1076,7 @@ int make_kv_attn_plan(const hk_shape *s, int64_t B, int64_t T, const hk_kv_cache
     p->off_prep = p->off_stats + align_up((size_t)p->M * sizeof(float2));
     p->off_partial = p->off_prep;
     if (p->M > 0 && hk::kv_gemm_uses_prepared(p->M, s->d, s->gemm_tile, s->dtype)) p->off_partial += prepared_layout(s->d).total;
-    const size_t floats = hk::kv_attn_partial_floats(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, c->total_tokens, s->attn_splits);
+    const size_t floats = hk::kv_attn_partial_floats(B, (int)T, s->n_heads, c->n_kv_heads, s->head_dim, codes, c->total_tokens, room, s->attn_splits);
     p->total = p->off_partial + align_up(floats * sizeof(float));
     return HK_OK;
 }

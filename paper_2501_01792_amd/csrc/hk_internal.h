@@ -260,8 +260,8 @@ struct KvAttnArgs {
     float scale;
 };
 // Scratch of the call, and whether its launches stay within what a launch can hold.
-size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits);
-bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits);
+size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int splits);
+bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int splits);
 // Attention of T query tokens a request over the cache, and over the nodes' own rows (see kv_attn_kernel.h).
 hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s);
 

@@ -149,13 +149,13 @@ hipError_t launch_merge(const Params &p, const Plan &pl, hipStream_t s)
 }  // namespace
 }  // namespace kvattn
 
-size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits)
+size_t kv_attn_partial_floats(int64_t B, int T, int H, int Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int splits)
 {
-    return (size_t)kvattn::plan(B, T, H, Hkv, head_dim, total_tokens, splits).partial_floats;
+    return (size_t)kvattn::plan(B, T, H, Hkv, head_dim, codes, total_tokens, room, splits).partial_floats;
 }
-bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, int64_t total_tokens, int splits)
+bool kv_attn_launchable(int64_t B, int T, int H, int Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int splits)
 {
-    const kvattn::Plan pl = kvattn::plan(B, T, H, Hkv, head_dim, total_tokens, splits);
+    const kvattn::Plan pl = kvattn::plan(B, T, H, Hkv, head_dim, codes, total_tokens, room, splits);
     // the launches of both forms and of their merges
     if (pl.shared) return pl.groups * (16 * kvattn::kWaves * pl.tiles / kvattn::kMergeRows) <= kvattn::kMostGroups;
     return pl.groups <= kvattn::kMostGroups && B * Hkv * pl.rows <= 4 * kvattn::kMostGroups;
@@ -165,7 +165,7 @@ hipError_t launch_kv_attn(const KvAttnArgs &a, hipStream_t s)
 {
     using namespace kvattn;
     if (a.B <= 0) return hipSuccess;
-    const Plan pl = plan(a.B, a.T, a.H, a.c.Hkv, a.head_dim, a.total_tokens, a.splits);
+    const Plan pl = plan(a.B, a.T, a.H, a.c.Hkv, a.head_dim, a.format != kvfmt::k16, a.total_tokens, (int64_t)a.c.max_blocks << a.c.blk_log2, a.splits);
     Params p;
     p.c = a.c;
     p.K_regen = a.K_regen; p.V_regen = a.V_regen; p.q = a.q; p.k = a.k; p.v = a.v;

@@ -42,7 +42,7 @@ struct Params {
     float scale_log2e;
 };
 
-// The streaming kernel in a cache's format; a translation unit each.
+// The kernels in a cache's format; a translation unit each.
 hipError_t launch_16(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
 hipError_t launch_int8(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
 hipError_t launch_e4m3(const Params &p, const Plan &pl, int head_dim, int dtype, hipStream_t s);
@@ -713,11 +713,8 @@ __device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_
     }
 }
 
-// Wavefronts of a SIMD that the registers are held to.
-constexpr int residency(int DH, int FMT, int MT) { return MT == 2 ? 2 : DH == 64 ? 4 : FMT == k16 ? 3 : 4; }
-
 template <int DH, int DT, int FMT, int MT, bool TREE>
-__global__ __launch_bounds__(kThreads, TREE ? 2 : residency(DH, FMT, MT)) void kv_attn_kernel(Params p)
+__global__ __launch_bounds__(kThreads, resident_pieces(DH, MT, FMT != k16, TREE)) void kv_attn_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
@@ -738,11 +735,10 @@ __global__ __launch_bounds__(kThreads, TREE ? 2 : residency(DH, FMT, MT)) void k
         }
     }
     if (!place(p, lane, at)) return;
-    constexpr int first_row = 0;
     if (p.slots > 0 && at.piece == 0 && at.h == 0 && threadIdx.x == 0) piece_notes(p, DH)[at.r] = make_int2(at.x, at.pieces);
     if (at.nodes <= 0) return;                             // no rows
     wave_t w;
-    w.rows(p, at, first_row, lane, TREE);
+    w.rows(p, at, 0, lane, TREE);
     w.scales = scales[FMT == k16 ? 0 : wave];
     w.clear();
     w.ask_q();

@@ -26,13 +26,31 @@ constexpr int kTileTokens = 32;                      // tokens a wavefront takes
 constexpr int kWaves = 4;
 constexpr int kStep = kTileTokens * kWaves;          // tokens of a round of a workgroup whose wavefronts share them out
 constexpr int kMaxTiles = 2;                         // tiles of 16 query rows in a wavefront
-constexpr int kWantGroups = 1024;                    // workgroups that fill the chip: 256 compute units x 4 (two tiles: x 2)
-constexpr int kWholeTokens = 512;                    // requests that short on average are not cut: the merge is a launch of its own
+constexpr int kUnits = 256;                          // compute units
 constexpr int kLeastRange = 4;                       // tiles of a range at least
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
-// Workgroups of a compute unit that the registers of the shared form leave room for.
+// Workgroups of a compute unit that the registers leave room for: the shared form, and the other one (`codes`: 8 bits, `tree`: nodes).
 HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 && tiles == 1 ? 3 : 2; }
+HK_HOST_DEVICE constexpr int resident_pieces(int head_dim, int tiles, bool codes, bool tree)
+{
+    return tiles == 2 ? 2 : head_dim == 64 ? 4 : tree ? 2 : codes ? 4 : 3;
+}
+
+// Are requests left whole (one piece each, no merge, which is a launch of its own) where attn_splits leaves the choice?
+//   * Where they are short: 512 tokens on average.  8 requests of 300 tokens and 8 K/V heads, int8: 7.6 us whole, 10.6 cut;
+//     16 bits at 560 tokens 10.3 and 10.7, at 1125 tokens 21.3 and 16.1; one request of 3000: 15.5 and 10.5.
+//   * Where they fill the chip, `want` workgroups.
+//   * Where they give every compute unit one and are of like length: what the cut gains in balance, its merge and its shorter
+//     pieces lose.  8 requests x 32 K/V heads, 560 / 1125 / 2250 / 6000 tokens on average (from half of the longest on), e4m3,
+//     one token: 11 / 19 / 35 / 86 us whole, 16 / 24 / 39 / 92 cut; 24 nodes over int8: 20 / 32 / 50 / 108 and 33 / 45 / 64 /
+//     131.  dh = 64 (25 requests x 12 heads, 12 nodes, 16 bits): 16 / 28 / 51 / 120 and 22 / 31 / 46 / 101.  Of like length:
+//     the table has no room for a request of more than four times the average.
+inline bool left_whole(int64_t B, int64_t Hkv, int head_dim, int64_t total_tokens, int64_t room, int64_t want)
+{
+    if (total_tokens <= 512 * B || B * Hkv >= want) return true;
+    return B * Hkv >= kUnits && total_tokens <= (head_dim == 64 ? 1536 : 8192) * B && room * B <= 4 * total_tokens;
+}
 
 struct Plan {
     int64_t rows;            // T * g
@@ -44,7 +62,8 @@ struct Plan {
     int64_t partial_floats;  // slots of head_dim sums, then of (m, l), then what the merge has to know of a request or range
 };
 
-inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int64_t total_tokens, int splits)
+// room: the longest request that the table has room for.
+inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int splits)
 {
     Plan p;
     p.rows = T * (H / Hkv);
@@ -56,17 +75,17 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, int
         const int64_t held = 16 * kWaves * p.tiles;
         // tiles of the line at most: those of the tokens, a last one of each request that is not full, two of nodes
         const int64_t line = (total_tokens / kTileTokens + 3 * B) * Hkv * ((p.rows + held - 1) / held);
-        const int64_t want = splits > 0 ? B * Hkv * splits : 256 * resident(head_dim, p.tiles);
+        const int64_t want = splits > 0 ? B * Hkv * splits : kUnits * resident(head_dim, p.tiles);
         const int64_t fit = (line + kLeastRange - 1) / kLeastRange;
         p.groups = want < fit ? want : fit > 0 ? fit : 1;
         p.slots = p.groups > 1 ? 2 * p.groups * held : 0;
     } else {
         p.tiles = (int)all;
         int64_t S = 0;
-        const int64_t want = kWantGroups / p.tiles;
+        const int64_t want = kUnits * resident_pieces(head_dim, p.tiles, codes, T > 1);
         if (splits > 0) {
             S = splits > 1 ? B * splits : 0;
-        } else if (B * Hkv < want && total_tokens > kWholeTokens * B) {
+        } else if (!left_whole(B, Hkv, head_dim, total_tokens, room, want)) {
             S = (want + Hkv - 1) / Hkv - B;
             const int64_t most = total_tokens / kStep;       // a piece has a round at least
             S = S < most ? S : most;

@@ -29,7 +29,8 @@ int main()
         }
         const int64_t bound = total + (rng() % 2 ? 0 : rng() % 100000);
         const int splits = rng() % 3 ? 0 : (int)(rng() % 65);
-        const Plan p = plan(B, T, (int64_t)Hkv * g, Hkv, dh, bound, splits);
+        const int64_t room = *std::max_element(len.begin(), len.end()) + (rng() % 2 ? 0 : rng() % 100000);
+        const Plan p = plan(B, T, (int64_t)Hkv * g, Hkv, dh, rng() % 2, bound, room, splits);
         const int held = p.tiles * 16 * (p.shared ? kWaves : 1);
         if (p.rows != T * g || p.tiles < 1 || p.tiles > kMaxTiles || (!p.shared && held < p.rows) || p.groups < 1) {
             std::printf("plan: rows %ld tiles %d groups %ld\n", (long)p.rows, p.tiles, (long)p.groups);
