@@ -1,5 +1,5 @@
 // Attention over the paged K/V cache: the launch of its kernels (kv_attn_kernel.h, kv_attn_rows.h) in the cache's format, and
-// the merge of the pieces that a request's tokens were cut into.
+// the merges of what they leave of requests whose tokens were cut.
 #include "kv_attn_kernel.h"
 #include "kv_attn_rows.h"
 
@@ -9,7 +9,8 @@ namespace {
 
 constexpr int kMergeBatch = 8;
 
-// Joins the pieces of a row: one wavefront each, DH / 64 elements a lane.
+// Joins the pieces of a row: one wavefront each, DH / 64 elements a lane.  A few KB a row, bound by one way to memory: the
+// loads of kMergeBatch pieces are on their way together (one request of 2000 tokens, 32 rows of 16 pieces: 4 us, which is what a launch and two ways to memory take).
 template <int DH, int DT>
 __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
 {
@@ -65,8 +66,11 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
 }
 
 // Joins the parts of a unit that more than one range of kv_attn_rows.h holds: kMergeRows rows of the unit whose second part
-// lies in range w.  A row is DH / 4 lanes, four elements each; a thread has all of its rows on their way.
-constexpr int kMergeRows = 32, kMergeThreads = 256;
+// lies in range w.  A row is DH / 4 lanes, four elements each.  It is bound by the way to memory: the parts come two and then four
+// at a time, and 16 rows a workgroup spread a unit of many parts (a long request) over more of them.  The whole call, int8, 8 K/V
+// heads: one request of 4000 tokens and 256 rows a head 35 us (32 rows a workgroup, one part at a time: 40), 64 rows over 1000
+// tokens 19.6 (21.8).  Eight at a time cost occupancy where units have few parts: 16 requests of 2000 tokens 86 for 78.
+constexpr int kMergeRows = 16, kMergeThreads = 256;
 
 template <int DH, int DT>
 __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, int held)
@@ -74,52 +78,54 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
     typedef typename Elem<DT>::T elem_t;
     typedef elem_t vec4_t __attribute__((ext_vector_type(4)));
     constexpr int LPR = DH / 4, RPB = kMergeThreads / LPR, kDeep = kMergeRows / RPB;
-    const int parts = held / kMergeRows, wg = blockIdx.x / parts + 1, part = blockIdx.x % parts;
+    const int blocks = held / kMergeRows, wg = blockIdx.x / blocks + 1, block = blockIdx.x % blocks;
     const int4 note = reinterpret_cast<const int4 *>(p.partial + p.slots * (DH + 2))[wg];
-    const int r = uniform(note.x), h = uniform(note.y), row0 = uniform(note.z) + part * kMergeRows, n_parts = uniform(note.w);
+    const int r = uniform(note.x), h = uniform(note.y), row0 = uniform(note.z) + block * kMergeRows, n_parts = uniform(note.w);
     if (n_parts == 0) return;                              // no unit whose second part begins this range
     const int len = length_of(p.c, r), nodes = nodes_of(p, r), rows = nodes * p.g;
+    if (row0 >= rows) return;
     const float *ml = p.partial + p.slots * DH;
     const int c = threadIdx.x % LPR, mine = threadIdx.x / LPR;
-    // the first part is that of range wg - 1, which begins the unit; the others do not
-    auto slot_of = [&](int x) { return (int64_t)(2 * x + (x == wg - 1)) * held + part * kMergeRows + mine; };
-    float2 v[2][kDeep];
-    float4_t s[2][kDeep];
-    auto ask = [&](int x, int b) {                         // also rows that there are not: what their slots hold is not used
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-            v[b][u] = *reinterpret_cast<const float2 *>(ml + 2 * (slot_of(x) + u * RPB));
-            s[b][u] = *reinterpret_cast<const float4_t *>(p.partial + (slot_of(x) + u * RPB) * DH + 4 * c);
-        }
-    };
     float m[kDeep], l[kDeep];
     float4_t o[kDeep];
-    auto add = [&](int b) {
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-            const float top = fmaxf(m[u], v[b][u].x), ref = top == -INFINITY ? 0.f : top;
-            const float f = __builtin_amdgcn_exp2f(m[u] - ref), g = __builtin_amdgcn_exp2f(v[b][u].x - ref);
-            l[u] = l[u] * f + v[b][u].y * g;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * f + s[b][u][e] * g;
-            m[u] = top;
-        }
-    };
-    ask(wg - 1, 0);                                        // two parts at least: both on their way at once
-    ask(wg, 1);
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
         m[u] = -INFINITY;
         l[u] = 0.f;
         o[u] = float4_t{0.f, 0.f, 0.f, 0.f};
     }
-    add(0);
-    add(1);
-    for (int x = wg + 1; x < wg - 1 + n_parts; ++x) {
-        ask(x, 0);
-        add(0);
-    }
-    if (row0 >= rows) return;
+    const int last = wg + n_parts - 2;                     // the range of the last part
+    auto join = [&](auto count, int x0) {                  // parts of ranges x0 .. x0 + count - 1, all on their way at once
+        constexpr int N = decltype(count)::value;
+        float2 v[N][kDeep];
+        float4_t s[N][kDeep];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            // the first part is that of range wg - 1, which begins the unit; the others do not
+            const int x = x0 + i;
+            const int64_t slot = (int64_t)(2 * x + (x == wg - 1)) * held + block * kMergeRows + mine;
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {              // also rows that there are not: what their slots hold is not used
+                v[i][u] = *reinterpret_cast<const float2 *>(ml + 2 * (slot + u * RPB));
+                s[i][u] = *reinterpret_cast<const float4_t *>(p.partial + (slot + u * RPB) * DH + 4 * c);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+                const float top = fmaxf(m[u], v[i][u].x), ref = top == -INFINITY ? 0.f : top;
+                const float f = __builtin_amdgcn_exp2f(m[u] - ref), g = __builtin_amdgcn_exp2f(v[i][u].x - ref);
+                l[u] = l[u] * f + v[i][u].y * g;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * f + s[i][u][e] * g;
+                m[u] = top;
+            }
+    };
+    join(std::integral_constant<int, 2>(), wg - 1);        // two parts at least
+    int x = wg + 1;
+    for (; x + 3 <= last; x += 4) join(std::integral_constant<int, 4>(), x);
+    for (; x <= last; ++x) join(std::integral_constant<int, 1>(), x);
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
         const int row = row0 + mine + u * RPB, node = row / p.g;

@@ -25,7 +25,8 @@ __device__ __forceinline__ constexpr float most() { return FMT == kInt8 ? 127.f 
 
 // 8 elements of a row -> 8 codes.  scale is finite and not below kLeastScale, inv = 1 / scale (rounded correctly, as the
 // language's division is).  x / scale rounded correctly comes from two multiply-adds on x inv, its residue times inv added on: the
-// last steps of a division, without the scaling that keeps a general one out of the ranges that cannot occur here.
+// last steps of a division, without the scaling that keeps a general one out of the ranges that cannot occur here.  (A
+// residue below fp32's normal numbers is off by 2^-150 at most: 2^-50 of a code at the least scale.)
 template <int FMT>
 __device__ __forceinline__ u32x2_t encode8(const float (&x)[8], float scale, float inv)
 {

@@ -25,12 +25,18 @@ namespace kvattn {
 constexpr int kTileTokens = 32;                      // tokens a wavefront takes at once
 constexpr int kWaves = 4;
 constexpr int kStep = kTileTokens * kWaves;          // tokens of a round of a workgroup whose wavefronts share them out
-constexpr int kMaxTiles = 2;                         // tiles of 16 query rows in a wavefront
+// Tiles of 16 query rows in a wavefront.  Three would need more registers than two workgroups a compute unit leave; at two the
+// streaming form is as fast as the shared one or faster (8 requests of up to 1024 tokens x 32 heads, 24 rows, int8: 26 and 36 us;
+// 16 requests of up to 2000, 32 rows on 8 K/V heads, 16 bits: 39 and 42).
+constexpr int kMaxTiles = 2;
 constexpr int kUnits = 256;                          // compute units
-constexpr int kLeastRange = 4;                       // tiles of a range at least
+// Tiles of a range at least: fewer cost more in beginnings and partial results than they gain in workgroups.  One request of
+// 1000 tokens, 64 rows on 8 K/V heads: 22.4 us with 4, 24.1 with 2, 23.7 with 8; 4 of 2000, 256 rows: 46.6, 46.4, 48.4.
+constexpr int kLeastRange = 4;
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
 // Workgroups of a compute unit that the registers leave room for: the shared form, and the other one (`codes`: 8 bits, `tree`: nodes).
+// (Three of the shared form's smaller one at dh = 128 spill: 33 rows 44 us for 37.)
 HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 && tiles == 1 ? 3 : 2; }
 HK_HOST_DEVICE constexpr int resident_pieces(int head_dim, int tiles, bool codes, bool tree)
 {
@@ -71,6 +77,8 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, boo
     p.shared = all > kMaxTiles;
     p.extra = 0;
     if (p.shared) {
+        // two tiles a wavefront where one leaves rows for another workgroup: 16 requests of up to 8192 tokens, 512 rows 353 us
+        // for 479, 16 of 2000, 256 rows 78 for 93 (small batches lose: 4 of 2000 45 for 41)
         p.tiles = all > kWaves ? 2 : 1;
         const int64_t held = 16 * kWaves * p.tiles;
         // tiles of the line at most: those of the tokens, a last one of each request that is not full, two of nodes

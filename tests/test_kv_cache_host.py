@@ -169,12 +169,12 @@ def test_workspace_is_known_before_the_pools_are():
 
 
 def test_cuts_that_no_launch_holds_are_refused():
-    """At most 2^23 workgroups of 256: the pieces of 8 K/V heads (one row), or 2^21 ranges that are merged by 4 (512 rows)."""
+    """At most 2^23 workgroups of 256: the pieces of 8 K/V heads (one row), or 2^20 ranges that are merged by 8 (512 rows)."""
     size = hk.lib().hk_kv_attn_workspace_bytes
     shape = hk.make_shape(4096, 32, attn_splits=64)
     ask = lambda B, T: size(ctypes.byref(shape), B, T, ctypes.byref(_cache(max_blocks=1 << 13, total_tokens=B << 17)))
     assert ask(16131, 1) > 0 and ask(16132, 1) == 0        # 16131 * 65 * 8 <= 2^23
-    assert ask(1 << 12, 64) > 0 and ask((1 << 12) + 1, 64) == 0
+    assert ask(1 << 11, 64) > 0 and ask((1 << 11) + 1, 64) == 0
 
 
 def test_struct_layout():
