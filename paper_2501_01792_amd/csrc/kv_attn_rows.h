@@ -12,7 +12,7 @@
 // in 309 us, 0.52 PFLOP/s (481 us with workgroups of equal requests instead of ranges, 850 with every wavefront making its own
 // operands).  A wavefront issues some 200 vector, 100 scalar and 32 matrix instructions a tile of 32 tokens x 32 rows, of which
 // 64 exponentials and conversions cannot go, and two wavefronts a SIMD are all that the registers (o alone 64) leave room for.
-// 33 nodes of 40 heads, e4m3, 7 requests of 383 to 1148 tokens: 36 us, some 14 tiles a workgroup, of which the beginning
+// 33 nodes of 40 heads, e4m3, 7 requests of 383 to 1148 tokens: 34 us, some 14 tiles a workgroup, of which the beginning
 // (lengths, table, queries, first rows: four ways to memory) and the merge (7) are the larger part.
 #pragma once
 #include "kv_attn_kernel.h"
