@@ -486,6 +486,40 @@ def test_two_graphs_that_share_a_workspace():
         assert torch.equal(out[0], got[0]) and torch.equal(out[1, :3], got[1, :3]) and torch.equal(out1, got1)
 
 
+@pytest.mark.parametrize("T,H", [(9, 8), (24, 8)])         # 36 and 96 rows on a K/V head: ranges of one tile of rows and of two
+def test_a_graph_of_ranges_follows_the_lengths(T, H):
+    """The cut of many rows is found on the device: one capture serves lengths and trees of every size."""
+    c = Cache(110, "e4m3", "bf16", [40, 700, 5], 2, 128, 16, max_blocks=64, spare=200, total=3 * 64 * 16)
+    c.dtable[:] = torch.arange(192, dtype=torch.int32).view(3, 64)
+    c.table = c.dtable.cpu().numpy()
+    q, k, v = (normal(111 + i, 3, T, h, 128, dtype="bf16") for i, h in enumerate((H, 2, 2)))
+    nodes, out = torch.full((3,), T, dtype=torch.int32).cuda(), torch.zeros_like(q)
+    ws = hk.new_workspace(hk.kv_attn_workspace_bytes(q, c.handle))
+    call = lambda: hk.kv_tree_attn(q, k, v, c.handle, n_nodes=nodes, out=out, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        call()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    torch.cuda.current_stream().wait_stream(side)
+    for lens, n in (([1000, 1, 33], [T, 1, T]), ([0, 0, 1024], [0, T, T - 1]), ([0, 0, 0], [0, 0, 0]), ([512, 640, 31], [T, T, T])):
+        c.lens = np.asarray(lens, np.int32)
+        c.dlens.copy_(torch.from_numpy(c.lens))
+        nodes.copy_(torch.tensor(n, dtype=torch.int32))
+        out.fill_(7.0)
+        torch.randn(1 << 20, device="cuda").sum()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        check_attention("ranges", c, q, k, v, None, n, got, untouched=7.0)
+        ws.fill_(0xff)
+        out.fill_(7.0)
+        call()
+        assert torch.equal(out, got)
+
+
 @pytest.mark.parametrize("form", ["int8", "e4m3", "16"])
 def test_speculative_decoding_over_a_quantised_cache(form):
     """The calls of a serving loop, in turn: prompts of different lengths are stored; each step drafts a tree whose Q, K, V come
