@@ -614,6 +614,8 @@ def make_kv_cache(K_pool, V_pool, block_table, seq_len, block_tokens, K_scale=No
         raise ValueError("K_scale, V_scale: [P_kv, n_kv_heads, block_tokens]")
     if act_pool is not None and (act_pool.dim() != 3 or act_pool.shape[1] != block_tokens):
         raise ValueError("act_pool: [P_act, block_tokens, d]")
+    if act_pool is not None and act_pool.shape[0] > 0 and act_pool.shape[2] != K_pool.shape[1] * K_pool.shape[3]:
+        raise ValueError("act_pool: d = n_kv_heads * dh (every query head of a layer with ACT blocks has a K/V head)")
     ptr, el = _dev_ptr, K_pool.dtype
     c = KvCache()
     c.tensors = (K_pool, V_pool, K_scale, V_scale, act_pool, block_table, seq_len)
