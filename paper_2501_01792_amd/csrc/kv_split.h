@@ -110,7 +110,7 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, boo
 HK_HOST_DEVICE inline int64_t piece_tokens(int64_t total, int64_t S)
 {
     if (S <= 0) return int64_t(1) << 40;
-    const int64_t C = (((uint64_t)total | (uint64_t)S) >> 32) == 0 ? (int64_t)(((uint32_t)total + (uint32_t)(S - 1)) / (uint32_t)S) : (total + S - 1) / S;
+    const int64_t C = ranges::quot(total + S - 1, S);
     return C < kStep ? kStep : (C + kStep - 1) / kStep * kStep;
 }
 
