@@ -420,7 +420,8 @@ int hk_paged_decode_attn_absorbed(const hk_shape *shape, const void *q, int32_t 
  *                with a 3-bit mantissa): the pools hold one byte an element and every (token, K/V head) has a scale of its
  *                own for K and for V; the element is scale * code.
  *   K_pool, V_pool    [P_kv, n_kv_heads, block_tokens, dh], elements of the format
- *   K_scale, V_scale  [P_kv, n_kv_heads, block_tokens] fp32, not negative; NULL for HK_KV_16
+ *   K_scale, V_scale  [P_kv, n_kv_heads, block_tokens] fp32; NULL for HK_KV_16.  hk_kv_store writes 2^-100 .. 2^121, or NaN; a
+ *                caller's own scales are 0 .. 2^121 (the attention takes one of V below 2^-100 as 2^-100)
  *   act_pool     [P_act, block_tokens, d] and table entries < 0 (ACT blocks): HK_KV_16 with n_kv_heads == n_heads only.  A
  *                checkpoint takes as many bytes as an 8-bit K/V row pair, so an 8-bit cache has nothing to win from ACT
  *                blocks: P_act must be 0 there (HK_ERR_SHAPE).

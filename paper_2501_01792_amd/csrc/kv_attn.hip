@@ -37,6 +37,8 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
             const float2 v = *reinterpret_cast<const float2 *>(ml + 2 * (slot0 + (i0 + lane) * step));
             w = __builtin_amdgcn_exp2f(v.x - ref);
             lw = w * v.y;
+            // over 8 bits the maxima hold scales of V, the denominators do not
+            if (__builtin_expect(is_far(v.x - ref), 0)) lw = times_power(v.y, v.x - ref);
         }
         for (int off = 32; off > 0; off >>= 1) lw += __shfl_xor(lw, off, 64);
         l += lw;
@@ -116,7 +118,10 @@ __global__ __launch_bounds__(kMergeThreads) void kv_rows_merge_kernel(Params p, 
             for (int u = 0; u < kDeep; ++u) {
                 const float top = fmaxf(m[u], v[i][u].x), ref = top == -INFINITY ? 0.f : top;
                 const float f = __builtin_amdgcn_exp2f(m[u] - ref), g = __builtin_amdgcn_exp2f(v[i][u].x - ref);
+                // over 8 bits the maxima hold scales of V, the denominators do not
+                const float d = fminf(m[u] - ref, v[i][u].x - ref), before = l[u];
                 l[u] = l[u] * f + v[i][u].y * g;
+                if (__builtin_expect(is_far(d), 0)) l[u] = m[u] < top ? v[i][u].y + times_power(before, d) : before + times_power(v[i][u].y, d);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[u][e] = o[u][e] * f + s[i][u][e] * g;
                 m[u] = top;

@@ -13,8 +13,10 @@
 //            each of those 8 tokens and turns the block with byte permutes; row a of product i is element a DH / 16 + i.
 //   8 bits   the scales are constants of a token: K's multiplies the score.  V's goes into the weight: with vs = mant 2^e,
 //            2^(t + e - m) mant <= 1 for the running maximum m of t + e, so the weight keeps fp16's 11 bits whatever the
-//            scales are, and the denominator takes 2^(t + e - m) 2^-e, in fp32.  A bf16 query is brought to fp16 by a power of
-//            two of its row.
+//            scales are, and the denominator takes 2^(t + e - m) 2^-e, in fp32.  Scales reach from 2^-100 (a row of zeros) to
+//            2^121, so that weight may be nothing in fp32 where the denominator's part is not: tiles with scales that far apart
+//            take count_far(), and factors between running maxima are kept from vanishing (times_power).  A bf16 query is brought to
+//            fp16 by a power of two of its row.
 // Up to 32 rows (kv_attn_kernel): a workgroup's 4 wavefronts take the 32-token tiles of a piece in turn, rows of K and V go from
 // memory to registers, and they join at the end in LDS.  More rows: kv_attn_rows.h.  A piece that is its request's only one
 // writes the output; the others leave (m, l, o) for the merge.
@@ -198,9 +200,20 @@ __device__ __forceinline__ float max_over_groups(float v)
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
+// 2^d below fp32's normal numbers, which the exponential gives as 0, is 2^-126 times 2^(d + 126).
+constexpr float kLeastPower = -126.f;
+__device__ __forceinline__ bool is_far(float d) { return d < kLeastPower && d > -INFINITY; }
+__device__ __forceinline__ float times_power(float v, float d)
+{
+    const bool far = d < kLeastPower;
+    return v * __builtin_amdgcn_exp2f(far ? d - kLeastPower : d) * (far ? 0x1p-126f : 1.f);
+}
+
 // The scales of a tile, one a lane (`sc`: K's in lanes 0 .. 31, V's in the others), as its scores and weights take them: [0, 32)
 // K's times the softmax scale, [32, 64) log2 of V's, [96, 128) the reciprocals of V's.  Tokens that do not exist (n0, n1 of the two
-// 16s do): 0 s - inf, and no part of the denominator.
+// 16s do): 0 s - inf, and no part of the denominator.  Returns whether a scale of V lies outside [kNearLow, kNearHigh]: among
+// scales within it a weight below fp32's numbers belongs to a token 62 binary orders below another one.
+constexpr float kNearLow = 0x1p-48f, kNearHigh = 0x1p16f;
 constexpr int kScales = 4 * kTileTokens;
 __device__ __forceinline__ const float *scale_at(const float *ks0, const float *ks1, const float *vs0, const float *vs1, int lane)
 {
@@ -209,7 +222,7 @@ __device__ __forceinline__ const float *scale_at(const float *ks0, const float *
     const uintptr_t a = lane & 16 ? k1 : k0, b = lane & 16 ? v1 : v0;
     return reinterpret_cast<const float *>(lane < 32 ? a : b) + (lane & 15);
 }
-__device__ __forceinline__ void put_scales(float *to, float sc, int n0, int n1, int lane, float scale)
+__device__ __forceinline__ uint32_t put_scales(float *to, float sc, int n0, int n1, int lane, float scale)
 {
     const int tok = lane & 31;
     const bool in = (tok & 15) < (tok < 16 ? n0 : n1);
@@ -217,6 +230,9 @@ __device__ __forceinline__ void put_scales(float *to, float sc, int n0, int n1, 
     const float lv = in ? __builtin_amdgcn_logf(v) : -INFINITY, kq = in ? sc * scale : 0.f;
     to[lane] = lane < 32 ? kq : lv;
     to[64 + lane] = in ? __builtin_amdgcn_rcpf(v) : 0.f;
+    // (the bits of positive floats order as they do; V's are those of the upper half of the wavefront)
+    constexpr uint32_t low = __builtin_bit_cast(uint32_t, kNearLow), high = __builtin_bit_cast(uint32_t, kNearHigh);
+    return (uint32_t)(__ballot(in && __builtin_bit_cast(uint32_t, v) - low > high - low) >> 32);
 }
 
 // Waits until at most N of this wavefront's loads are on their way.
@@ -252,6 +268,7 @@ struct Wave {
     uint64_t seen[MT];                                     // nodes that it sees
     float scale;                                           // scale * log2(e)
     int g4, r16, some;                                     // some: bit mt: the row sees something
+    uint32_t wide;                                         // 8 bits, not 0: scales of V far apart have been met (wavefront-uniform)
 
     // Reduction elements of product kk that this lane holds: 8 from here on.
     __device__ __forceinline__ int k_elem(int kk) const
@@ -320,6 +337,7 @@ struct Wave {
     }
     __device__ __forceinline__ void clear()
     {
+        wide = 0;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             m[mt] = -INFINITY;
@@ -343,9 +361,14 @@ struct Wave {
         if (__ballot(any)) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const float alpha = behind[mt] ? __builtin_amdgcn_exp2f(m[mt] - top[mt]) : 1.f;
-                m[mt] = behind[mt] ? top[mt] : m[mt];
+                const float d = m[mt] - top[mt], alpha = behind[mt] ? __builtin_amdgcn_exp2f(d) : 1.f;
+                const float before = l[mt];
                 l[mt] *= alpha;
+                if constexpr (FMT != k16) {                // m holds V's scale, l does not
+                    const bool far = behind[mt] && is_far(d);
+                    if (__builtin_expect(__ballot(far) != 0, 0)) l[mt] = far ? times_power(before, d) : l[mt];
+                }
+                m[mt] = behind[mt] ? top[mt] : m[mt];
 #pragma unroll
                 for (int i = 0; i < NI; ++i) o[mt][i] *= alpha;
             }
@@ -366,6 +389,29 @@ struct Wave {
             if constexpr (FMT == k16) top[mt] *= scale;
         }
         follow(top, ref);
+    }
+    // 8 bits, scales of V far apart: the part in the denominator of weights that are below fp32's numbers, which are then nothing.
+    __device__ __forceinline__ void count_far(float4_t (&t)[MT][2], const float4_t (&inv)[2], const float (&ref)[MT])
+    {
+        bool any = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float low = t[mt][0][0];
+#pragma unroll
+            for (int u = 1; u < 8; ++u) low = fminf(low, t[mt][u >> 2][u & 3]);
+            any = any || low - ref[mt] < kLeastPower;
+        }
+        if (__ballot(any) == 0) return;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float d = t[mt][u >> 2][u & 3] - ref[mt];
+                const bool far = d < kLeastPower;
+                l[mt] += far ? __builtin_amdgcn_exp2f(d - kLeastPower) * inv[u >> 2][u & 3] * 0x1p-126f : 0.f;
+                t[mt][u >> 2][u & 3] = far ? -INFINITY : t[mt][u >> 2][u & 3];
+                __builtin_amdgcn_sched_barrier(0);         // one by one: no registers for what is rare
+            }
     }
     // The weights as the product with V takes them, and their part in the denominator.
     __device__ __forceinline__ void weigh(int mt, const float4_t (&t)[2], const float4_t (&inv)[2], float ref, mvec8_t &pf)
@@ -397,7 +443,14 @@ struct Wave {
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const float w = __builtin_amdgcn_exp2f(t[mt][u >> 2][u & 3] - ref[mt]);
+                const float d = t[mt][u >> 2][u & 3] - ref[mt];
+                float w = __builtin_amdgcn_exp2f(d);
+                if constexpr (FMT != k16) {
+                    if (__builtin_expect(wide != 0, 0)) {  // the maximum may hold a scale of V up to 2^121
+                        w = times_power(1.f, d);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
                 t[mt][u >> 2][u & 3] = w;
                 l[mt] += w;
                 pf[mt][u] = (elem_t)w;
@@ -503,7 +556,7 @@ struct Wave {
     __device__ __forceinline__ void take(const int (&n)[2], const Tokens &next)
     {
         float4_t t[MT][2], inv[2];
-        if constexpr (FMT != k16) put_scales(scales, sc, n[0], n[1], 16 * g4 + r16, scale);
+        if constexpr (FMT != k16) wide |= put_scales(scales, sc, n[0], n[1], 16 * g4 + r16, scale);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             mvec8_t kf[KK];
@@ -553,6 +606,9 @@ struct Wave {
         mvec8_t pf[MT];
         float ref[MT];
         references(t, ref);
+        if constexpr (FMT != k16) {
+            if (__builtin_expect(wide != 0, 0)) count_far(t, inv, ref);
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) weigh(mt, t[mt], inv, ref[mt], pf[mt]);
         constexpr int G = FMT == k16 ? 2 : 4;
@@ -723,8 +779,12 @@ __device__ __forceinline__ void tokens_at(const Params &p, int h, int t0, int t_
     }
 }
 
+// Workgroups a compute unit that the registers are held to: resident_pieces(), or the third one that fp16 rows leave room for at
+// dh = 64 and two tiles (167 registers; the compiler's own choice is 177, which ends at two).
+constexpr int held_to(int DH, int DT, bool codes, int MT, bool tree) { return DH == 64 && MT == 2 && DT == 0 ? 3 : resident_pieces(DH, MT, codes, tree); }
+
 template <int DH, int DT, int FMT, int MT, bool TREE>
-__global__ __launch_bounds__(kThreads, resident_pieces(DH, MT, FMT != k16, TREE)) void kv_attn_kernel(Params p)
+__global__ __launch_bounds__(kThreads, held_to(DH, DT, FMT != k16, MT, TREE)) void kv_attn_kernel(Params p)
 {
     typedef Wave<DH, DT, FMT, MT> wave_t;
     typedef typename wave_t::elem_t elem_t;
@@ -806,10 +866,20 @@ __global__ __launch_bounds__(kThreads, resident_pieces(DH, MT, FMT != k16, TREE)
 #pragma unroll
         for (int q = 0; q < kWaves; ++q) top = fmaxf(top, join_ml[q][row][0]);
         const float ref = top == -INFINITY ? 0.f : top;
+        bool far = false;
 #pragma unroll
         for (int q = 0; q < kWaves; ++q) {
-            f[q] = __builtin_amdgcn_exp2f(join_ml[q][row][0] - ref);
+            const float d = join_ml[q][row][0] - ref;
+            f[q] = __builtin_amdgcn_exp2f(d);
             l = __builtin_fmaf(join_ml[q][row][1], f[q], l);
+            far = far || is_far(d);
+        }
+        if constexpr (FMT != k16) {
+            if (__builtin_expect(__ballot(far) != 0, 0)) { // as in follow()
+                l = 0.f;
+#pragma unroll
+                for (int q = 0; q < kWaves; ++q) l += times_power(join_ml[q][row][1], join_ml[q][row][0] - ref);
+            }
         }
         float4_t sum[NQ];
 #pragma unroll

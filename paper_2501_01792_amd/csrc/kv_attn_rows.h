@@ -91,8 +91,8 @@ struct Part {
         return n > 0 ? (uint32_t)(n - 1) * r.pitch + RB : 0;
     }
 
-    // n0, n1: as the rows were asked for.
-    __device__ __forceinline__ void put(Operands<DH> &to, int n0, int n1, int wave, int lane, float scale) const
+    // n0, n1: as the rows were asked for.  Returns what put_scales does.
+    __device__ __forceinline__ uint32_t put(Operands<DH> &to, int n0, int n1, int wave, int lane, float scale) const
     {
         if (!kSplit || wave < 2) {
             const int j = k_sixteen(wave);
@@ -141,8 +141,9 @@ struct Part {
         }
         if constexpr (kCodes) {
             // every wavefront stores the same: a branch would part the products from what runs under them
-            put_scales(to.scales, sc, n0, n1, lane, scale);
+            return put_scales(to.scales, sc, n0, n1, lane, scale);
         }
+        return 0;
     }
     // Infinities and NaN of V become zeros (16-bit rows); whether there were any.
     template <int DT>
@@ -280,12 +281,13 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
         };
         auto put = [&](const Part<DH, FMT> &from, int t, Operands<DH> &to) {
             const int here = at.t_end - t;
-            from.put(to, here < 16 ? here : 16, here < 16 ? 0 : here < 32 ? here - 16 : 16, wave, lane, w.scale);
+            const uint32_t far = from.put(to, here < 16 ? here : 16, here < 16 ? 0 : here < 32 ? here - 16 : 16, wave, lane, w.scale);
+            if constexpr (FMT != k16) w.wide |= far;
         };
         // One tile: its successor's operands are made from `next`, which then waits for the tile two behind that.  A wavefront
         // whose rows do not exist only makes operands.
         const bool mine = first_row < at.nodes * p.g;
-        auto tile = [&](auto has_rows, int tb, const Operands<DH> &op, Operands<DH> &op_next, Part<DH, FMT> &next) {
+        auto tile = [&](auto has_rows, int tb, const Operands<DH> &op, Operands<DH> &op_next, Part<DH, FMT> &next) __attribute__((always_inline)) {
             if constexpr (!decltype(has_rows)::value) {
                 put(next, tb + kTileTokens, op_next);
             } else {
@@ -337,6 +339,9 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
                 mvec8_t pf[MT];
                 float ref[MT];
                 w.references(t, ref);
+                if constexpr (FMT != k16) {
+                    if (__builtin_expect(w.wide != 0, 0)) w.count_far(t, inv, ref);
+                }
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {                  // one tile's products run under the next one's weights
                     w.weigh(mt, t[mt], inv, ref[mt], pf[mt]);
@@ -362,7 +367,7 @@ __global__ __launch_bounds__(kThreads, resident(DH, MT)) void kv_rows_kernel(Par
             ask(part[0], ent);
             entries_of(tab, t_ask, at.t_end, p.c.blk_log2, ent);
             meet();
-            auto tiles = [&](auto has_rows) {
+            auto tiles = [&](auto has_rows) __attribute__((always_inline)) {
                 int tb = at.t_begin;
                 do {
                     tile(has_rows, tb, ops[0], ops[1], part[1]);
