@@ -464,6 +464,8 @@ typedef struct hk_kv_cache {
  * gets the scale NaN and reads back as NaN.  HK_KV_16 rows are copied.
  * Only the rows of new tokens are written; tokens before 0 or behind the table's row, and entries outside the pools, are
  * not.  Requests that share a block must not write the same token in one call.  k and v may be NULL together when P_kv == 0.
+ * A launch holds B * (T + 15) * n_kv_heads <= 2^27; more is HK_ERR_SHAPE (as are 64 prompts of 32768 tokens with 72 heads): such
+ * a caller stores the requests in several calls, with block_table, seq_len and rows that begin at a later request.
  */
 int hk_kv_store(const hk_shape *shape, const void *k, const void *v, const void *x, int32_t B, int32_t T,
                 const int32_t *n_new, const int32_t *pick, const hk_kv_cache *cache, void *stream);
@@ -473,6 +475,8 @@ int hk_kv_store(const hk_shape *shape, const void *k, const void *v, const void 
  * as scale * code rounded once to the shape's dtype.
  *   K_out, V_out  [B, n_kv_heads, L_cap, dh], the shape's dtype: the layout of K_cache, V_cache of hk_hybrid_decode_attn
  * Other rows, and rows of tokens that sit in ACT blocks, are left as they are.
+ * A launch holds B * n_kv_heads * ceil(L_cap / 32) <= 2^23; more is HK_ERR_SHAPE: such a caller reads the tokens in several
+ * calls, tok_off after tok_off, into outputs of their own.
  */
 int hk_kv_load(const hk_shape *shape, void *K_out, void *V_out, int32_t B, int32_t tok_off, int32_t L_cap,
                const hk_kv_cache *cache, void *stream);
@@ -484,7 +488,12 @@ int hk_kv_load(const hk_shape *shape, void *K_out, void *V_out, int32_t B, int32
  *   q, out     [B, n_heads, dh]
  *   workspace  hk_kv_attn_workspace_bytes(shape, B, 1, cache); scratch only, nothing in it needs clearing
  * The probabilities are held in fp32; for the product with V they are rounded to the shape's dtype (HK_KV_16), or, taken
- * times the scales of V and relative to their running maximum, to fp16 (8-bit formats).
+ * times the scales of V and relative to their running maximum, to fp16 (8-bit formats).  fp16 is off by up to 2^-25 of the
+ * largest weight there, also where that is more than half a step.  A bf16 query meets 8-bit rows as fp16, divided by a power of
+ * two of its row: elements below 2^-17 of the row's largest are off by up to 2^-24 of it.
+ * A launch holds 2^23 workgroups, else HK_ERR_SHAPE (the workspace query returns 0 then): up to 32 query rows T * n_heads /
+ * n_kv_heads about B * n_kv_heads * max(attn_splits, 1) of them, and B * T * n_heads <= 2^25; beyond 32 rows
+ * B * n_kv_heads * attn_splits <= 2^20 (2^21 up to 64 rows).
  */
 size_t hk_kv_attn_workspace_bytes(const hk_shape *shape, int32_t B, int32_t T, const hk_kv_cache *cache);
 int hk_kv_decode_attn(const hk_shape *shape, const void *q, int32_t B, const hk_kv_cache *cache,

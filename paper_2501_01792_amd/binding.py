@@ -697,7 +697,8 @@ def _kv_on(cache, stream, call):
 def kv_store(cache, k, v, x=None, n_new=None, pick=None, stream=None):
     """hk_kv_store: the rows ``k, v[B, T, n_kv_heads, dh]`` of new tokens into the cache, the last ``n_new[b]`` (int32; default
     T) of the ``seq_len[b]`` tokens of each request, quantised where the pools hold 8 bits.  ``pick[B, T]`` int32: the row of
-    each new token (the accepted path of a tree).  ``x[B, T, d]``: layer inputs, stored where the block is an ACT block."""
+    each new token (the accepted path of a tree).  ``x[B, T, d]``: layer inputs, stored where the block is an ACT block.
+    A call holds B * (T + 15) * n_kv_heads <= 2^27; larger batches are stored in parts, a handle each on a slice of the requests."""
     import torch
     if k.dim() != 4:
         raise ValueError("k, v: [B, T, n_kv_heads, dh]")
@@ -715,7 +716,7 @@ def kv_store(cache, k, v, x=None, n_new=None, pick=None, stream=None):
 def kv_load(cache, L_cap, tok_off=0, dtype=None, K_out=None, V_out=None, stream=None):
     """hk_kv_load: tokens ``tok_off .. tok_off + L_cap - 1`` of every request as ``K, V[B, n_kv_heads, L_cap, dh]`` in ``dtype``
     (default: that of ``K_out``, of 16-bit pools, or float16).  Rows without a cached token are left as they are, zeros where
-    the outputs are allocated here."""
+    the outputs are allocated here.  A call holds B * n_kv_heads * ceil(L_cap / 32) <= 2^23; more is read in parts."""
     import torch
     if dtype is None:
         dtype = K_out.dtype if K_out is not None else cache.pool_dtype if cache.struct.format == HK_KV_16 else torch.float16
