@@ -426,7 +426,8 @@ int hk_paged_decode_attn_absorbed(const hk_shape *shape, const void *q, int32_t 
  *                checkpoint takes as many bytes as an 8-bit K/V row pair, so an 8-bit cache has nothing to win from ACT
  *                blocks: P_act must be 0 there (HK_ERR_SHAPE).
  *   total_tokens HOST: the sum of seq_len or any upper bound of it (at most B * max_blocks * block_tokens); it sizes the
- *                launch and the workspace of the attention, and changes no result but by the order of sums
+ *                launch and the workspace of the attention, and changes no result but by the order of sums.  The work is cut by
+ *                the lengths that the device holds; the nearer the bound, the better the host sees where no cut is needed
  * Table and lengths are device data: entries are held to the pools, lengths to the table's row, negative lengths count
  * as 0, so inconsistent tables give wrong numbers, not stray accesses.
  * These calls take every dtype of the shape and every format; hk_shape.attn_splits and gemm_tile as everywhere

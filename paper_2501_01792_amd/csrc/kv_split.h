@@ -43,19 +43,35 @@ HK_HOST_DEVICE constexpr int resident_pieces(int head_dim, int tiles, bool codes
     return tiles == 2 ? 2 : head_dim == 64 ? 4 : tree ? 2 : codes ? 4 : 3;
 }
 
+constexpr int64_t kWholeBytes = 1 << 20, kMostSearched = 512;
+
 // Are requests left whole (one piece each, no merge, which is a launch of its own) where attn_splits leaves the choice?
-//   * Where they are short: 512 tokens on average.  8 requests of 300 tokens and 8 K/V heads, int8: 7.6 us whole, 10.6 cut;
-//     16 bits at 560 tokens 10.3 and 10.7, at 1125 tokens 21.3 and 16.1; one request of 3000: 15.5 and 10.5.
+// Not where one of them may be long among short ones: a workgroup per K/V head would walk it alone (us, whole / cut: one request of
+// 12288 tokens among 32 of 128, 32 K/V heads, 16 bits 184 / 58; 32768 among 127 of 1000, 8 K/V heads, int8 278 / 74; 30000 among 63
+// of 40 217 / 27; lengths from 64 to 8192, as many in each octave, 128 requests 146 / 114).  The host knows the table's width and the
+// sum of the lengths, or a bound of it, so it is ruled out where
+//   * the longest that there can be has 1 MB of K and V at most, or
+//   * it has at most four times a request's share of the tokens, or, with more requests than that, a resident workgroup's share.
+//     A sum that is no less than all the table has room for says nothing.
+// What that costs where lengths are alike all the same (the table wide, the sum unknown or small): 128 requests of 250 to 500
+// tokens on 8 K/V heads, int8 23 / 27; 25 x 12 heads, 12 nodes, 16 bits 11 / 17.  Beyond 512 requests every workgroup's search for
+// its piece costs more than that: 1024 of 250 to 500 140 / 200, one of 32768 among them 368 / 241; so these are left alone.
+// Where it is ruled out:
+//   * Short requests are left whole, 512 tokens on average.  8 requests of 300 tokens and 8 K/V heads, int8: 6.7 us whole, 10.2
+//     cut; one request of 3000: 15.5 and 10.5.
 //   * Where they fill the chip, `want` workgroups.
-//   * Where they give every compute unit one and are of like length: what the cut gains in balance, its merge and its shorter
-//     pieces lose.  8 requests x 32 K/V heads, 560 / 1125 / 2250 / 6000 tokens on average (from half of the longest on), e4m3,
-//     one token: 11 / 19 / 35 / 86 us whole, 16 / 24 / 39 / 92 cut; 24 nodes over int8: 20 / 32 / 50 / 108 and 33 / 45 / 64 /
-//     131.  dh = 64 (25 requests x 12 heads, 12 nodes, 16 bits): 16 / 28 / 51 / 120 and 22 / 31 / 46 / 101.  Of like length:
-//     the table has no room for a request of more than four times the average.
-inline bool left_whole(int64_t B, int64_t Hkv, int head_dim, int64_t total_tokens, int64_t room, int64_t want)
+//   * Where they give every compute unit one: what the cut gains in balance, its merge and its shorter pieces lose.  8 requests x
+//     32 K/V heads, 560 / 1125 / 2250 / 6000 tokens on average (from half of the longest on), e4m3, one token: 11 / 19 / 35 / 86 us
+//     whole, 16 / 24 / 39 / 92 cut; 24 nodes over int8: 20 / 32 / 50 / 108 and 33 / 45 / 64 / 131.  dh = 64 (25 requests x 12 heads, 12
+//     nodes, 16 bits): 16 / 28 / 51 / 120 and 22 / 31 / 46 / 101.
+inline bool left_whole(int64_t B, int64_t Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int64_t want)
 {
+    const int64_t longest = room < total_tokens ? room : total_tokens, shares = B * Hkv < want ? B : (want + Hkv - 1) / Hkv;
+    const bool small = longest * head_dim * (codes ? 2 : 4) <= kWholeBytes;
+    const bool alike = total_tokens < room * B && room * shares <= 4 * total_tokens;
+    if (!small && !alike && B <= kMostSearched) return false;
     if (total_tokens <= 512 * B || B * Hkv >= want) return true;
-    return B * Hkv >= kUnits && total_tokens <= (head_dim == 64 ? 1536 : 8192) * B && room * B <= 4 * total_tokens;
+    return B * Hkv >= kUnits && total_tokens <= (head_dim == 64 ? 1536 : 8192) * B;
 }
 
 struct Plan {
@@ -93,8 +109,10 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, boo
         const int64_t want = kUnits * resident_pieces(head_dim, p.tiles, codes, T > 1);
         if (splits > 0) {
             S = splits > 1 ? B * splits : 0;
-        } else if (!left_whole(B, Hkv, head_dim, total_tokens, room, want)) {
+        } else if (!left_whole(B, Hkv, head_dim, codes, total_tokens, room, want)) {
             S = (want + Hkv - 1) / Hkv - B;
+            const int64_t few = (want / 2 + Hkv - 1) / Hkv;  // a piece has two resident workgroups' shares of the tokens at most
+            S = S > few ? S : few;
             const int64_t most = total_tokens / kStep;       // a piece has a round at least
             S = S < most ? S : most;
         }

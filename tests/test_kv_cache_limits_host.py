@@ -68,3 +68,10 @@ def test_requests_that_one_attention_holds(T, H, splits, B):
     shape = hk.make_shape(H * 128, H, attn_splits=splits)
     size = lambda B: hk.lib().hk_kv_attn_workspace_bytes(ctypes.byref(shape), B, T, ctypes.byref(_cache(max_blocks=512 if splits else 8, total_tokens=B * 8192 if splits else 0)))
     assert size(B) > 0 and size(B + 1) == 0
+
+
+def test_no_workgroup_walks_a_long_request_alone(tmp_path):
+    exe = str(tmp_path / "kv_split_skew_check")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", os.path.join(ROOT, "tests", "host", "kv_split_skew_check.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
