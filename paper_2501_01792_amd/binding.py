@@ -781,7 +781,8 @@ def _kv_attend(where, q, size, rows, tail, cache, layer_params, out, workspace, 
 def kv_decode_attn(q, cache, layer_params=None, out=None, workspace=None, softmax_scale=0.0, attn_splits=0, stream=None,
                    ln_eps=1e-5):
     """hk_kv_decode_attn: the query ``q[B, H, dh]`` of one token a request over the ``seq_len[b]`` tokens of the cache ->
-    ``out[B, H, dh]``.  H is a multiple of the cache's n_kv_heads.  ``layer_params`` as everywhere, for ACT blocks."""
+    ``out[B, H, dh]``.  H is a multiple of the cache's n_kv_heads.  ``layer_params`` as everywhere, for ACT blocks.  For 16-bit
+    caches with as many K/V heads as query heads ``paged_decode_attn`` is the faster call."""
     if q.dim() != 3:
         raise ValueError("q: [B, H, dh]")
     return _kv_attend("hk_kv_decode_attn", q, (cache.B, q.shape[1], cache.head_dim), (), (), cache, layer_params, out, workspace,

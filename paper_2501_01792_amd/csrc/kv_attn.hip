@@ -70,8 +70,8 @@ __global__ __launch_bounds__(256) void kv_merge_kernel(Params p)
 // Joins the parts of a unit that more than one range of kv_attn_rows.h holds: kMergeRows rows of the unit whose second part
 // lies in range w.  A row is DH / 4 lanes, four elements each.  It is bound by the way to memory: the parts come two and then four
 // at a time, and 16 rows a workgroup spread a unit of many parts (a long request) over more of them.  The whole call, int8, 8 K/V
-// heads: one request of 4000 tokens and 256 rows a head 35 us (32 rows a workgroup, one part at a time: 40), 64 rows over 1000
-// tokens 19.6 (21.8).  Eight at a time cost occupancy where units have few parts: 16 requests of 2000 tokens 86 for 78.
+// heads: one request of 4000 tokens and 256 rows a head 48 us (32 rows a workgroup, one part at a time: 52), 64 rows over 1000
+// tokens 21.8 (24.3).  Eight at a time cost occupancy where units have few parts: 16 requests of 2000 tokens 79 for 75.
 constexpr int kMergeRows = 16, kMergeThreads = 256;
 
 template <int DH, int DT>

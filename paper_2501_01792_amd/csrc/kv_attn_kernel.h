@@ -21,9 +21,9 @@
 // memory to registers, and they join at the end in LDS.  More rows: kv_attn_rows.h.  A piece that is its request's only one
 // writes the output; the others leave (m, l, o) for the merge.
 //
-// What bounds the streaming form is memory: 64 requests of up to 4096 tokens, 72 heads of 128, e4m3, bf16 (3.8 GB): 606 us, 6.28
-// TB/s; 16 bits, 8 query heads on each of 8 K/V heads, 4 requests of 16384 to 32768 tokens (375 MB): 68 us, 5.5 TB/s; int8, 32
-// requests x 32 heads of 512 to 1024 tokens (211 MB): 42 us, 5.0 TB/s, the longest requests' last rounds with ever fewer of them
+// What bounds the streaming form is memory: 64 requests of up to 4096 tokens, 72 heads of 128, e4m3, bf16 (3.8 GB): 607 us, 6.27
+// TB/s; 16 bits, 8 query heads on each of 8 K/V heads, 4 requests of 16384 to 32768 tokens (375 MB): 69 us, 5.4 TB/s; int8, 32
+// requests x 32 heads of 512 to 1024 tokens (211 MB): 43 us, 4.9 TB/s, the longest requests' last rounds with ever fewer of them
 // on the chip.  So a wavefront keeps a whole tile on its way while it takes one in: the loop asks for the next rows as registers
 // fall free, the table entry of the one after by a scalar load, and nothing in it waits for more than it uses (1064 us for the
 // first of these before).  Rows that one workgroup reads are loaded non-temporal: caches of several layers leave nothing of them
@@ -244,7 +244,7 @@ __device__ __forceinline__ void wait_loads()
 }
 
 // How far the running maximum may lag behind, in the log2 domain: weights stay below 2^kLag, far inside fp16, and most tiles move
-// no sums.  0 instead: 16 requests of up to 8192 tokens, 512 rows on a K/V head 369 us for 353.
+// no sums.  0 instead: 16 requests of up to 8192 tokens, 512 rows on a K/V head 376 us for 354.
 constexpr float kLag = 8.f;
 
 template <int DH, int DT, int FMT, int MT>

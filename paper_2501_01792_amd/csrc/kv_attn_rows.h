@@ -1,19 +1,21 @@
 // The form of kv_attn_kernel.h for many query rows (trees, shared K/V heads): the 4 wavefronts of a workgroup take 16 MT rows
 // each and share every tile of 32 tokens through LDS.
 //
-// There the vector ALU is the bound: a weight costs some ten instructions and an exponential, and making operands of the
-// rows of K and V (widening codes, turning V) costs as much as 16 to 32 query rows do.  So a wavefront makes a quarter of a
+// There the products are no longer what costs: a weight takes some ten vector instructions and an exponential, and making operands
+// of the rows of K and V (widening codes, turning V) as many as 16 to 32 query rows do.  So a wavefront makes a quarter of a
 // tile's operands and stores them in LDS in the order in which the matrix instructions read them, a lane's 16 bytes beside
 // its neighbour's; every wavefront reads them all.  Two buffers and one barrier a tile: while a tile is taken in, the next one's
 // operands are stored, and the rows of the two behind that are on their way from memory.
 // The wavefronts never join: each has all tokens of its rows.  How the work is cut into ranges is in kv_split.h.
 //
 // 16 requests of 4096 to 8192 tokens, 64 nodes, 8 query heads on each of 8 K/V heads of 128, int8, bf16: 1.6e11 products and sums
-// in 309 us, 0.52 PFLOP/s (481 us with workgroups of equal requests instead of ranges, 850 with every wavefront making its own
-// operands).  A wavefront issues some 200 vector, 100 scalar and 32 matrix instructions a tile of 32 tokens x 32 rows, of which
-// 64 exponentials and conversions cannot go, and two wavefronts a SIMD are all that the registers (o alone 64) leave room for.
-// 33 nodes of 40 heads, e4m3, 7 requests of 383 to 1148 tokens: 34 us, some 14 tiles a workgroup, of which the beginning
-// (lengths, table, queries, first rows: four ways to memory) and the merge (7) are the larger part.
+// in 314 us, 0.51 PFLOP/s (481 us with workgroups of equal requests instead of ranges, 850 with every wavefront making its own
+// operands).  No unit is full (counters, of the time that the wavefronts are there, two a SIMD, which is all that the registers, o
+// alone 64, leave room for): a SIMD's vector ALU works 62 %, its matrix core 28 %, and of a wavefront's time 46 % issues
+// an instruction, 29 % has one ready that waits for its turn, 24 % waits for a barrier, LDS or memory.
+// 33 nodes of 40 heads, e4m3, 7 requests of 383 to 1148 tokens: 36 us, some 14 tiles a workgroup; wavefronts wait 47 % of their
+// time, at the beginning (lengths, table, queries, first rows: four ways to memory) above all, and the merge takes 7.  Where a
+// request has few of the T nodes, wavefronts whose rows do not exist only make operands.
 #pragma once
 #include "kv_attn_kernel.h"
 

@@ -3,11 +3,12 @@
 // largest magnitude of a row is found among its lanes, as the integer that its bits are, so that infinities and NaN order
 // above every finite value.
 //
-// Memory bounds both: prompts of 8 requests of 1024 to 2048 tokens, 8 heads of 128, bf16 to e4m3 and back again 31 us, 136 MB at
-// 4.3 TB/s; read back alone, int8, 32 requests x 32 heads of 512 to 1024 tokens 122 us, 618 MB at 5.1 TB/s, a copy's rate (4.98).
-// Rows leave non-temporal (147 us for that batch without).  What the quantisation costs is kept below that: the quotients take
-// two multiply-adds each where a division takes ten instructions (prompts written at 3.7 TB/s with it, 4.7 without).  Small
-// calls are a launch (3.5 us) and the host's 6.
+// Memory bounds both.  Alone, over 814 MB (32 requests x 32 heads x 1024 tokens): written 4.7 TB/s (int8) and 5.0 (e4m3), 5.6 in 16
+// bits; read back 5.6, 5.5 and 5.5.  A copy of 1 GiB reaches 5.2, a fill 6.8: what a mixture of reads and writes reaches lies
+// between, by its shares.  Prompts of 8 requests of 1024 to 2048 tokens, 8 heads of 128, bf16 to e4m3 and back again 31 us, 136 MB.
+// Rows leave non-temporal (147 us without, for 122, where 32 requests x 32 heads of 512 to 1024 tokens are read back).  What the
+// quantisation costs is kept small: the quotients take two multiply-adds each where a division takes ten instructions (prompts
+// written at 3.7 TB/s with it, 4.7 without).  Small calls are a launch (3.4 us) and the host's 6.
 #include "hk_internal.h"
 #include "kv_format.h"
 

@@ -26,17 +26,19 @@ constexpr int kTileTokens = 32;                      // tokens a wavefront takes
 constexpr int kWaves = 4;
 constexpr int kStep = kTileTokens * kWaves;          // tokens of a round of a workgroup whose wavefronts share them out
 // Tiles of 16 query rows in a wavefront.  Three would need more registers than two workgroups a compute unit leave; at two the
-// streaming form is as fast as the shared one or faster (8 requests of up to 1024 tokens x 32 heads, 24 rows, int8: 26 and 36 us;
-// 16 requests of up to 2000, 32 rows on 8 K/V heads, 16 bits: 39 and 42).
+// streaming form is as fast as the shared one or faster (8 requests of up to 1024 tokens x 32 heads, 24 rows, int8: 27 and 35 us;
+// 16 requests of 2000, 32 rows on 8 K/V heads, 16 bits: 39 and 40).
 constexpr int kMaxTiles = 2;
 constexpr int kUnits = 256;                          // compute units
-// Tiles of a range at least: fewer cost more in beginnings and partial results than they gain in workgroups.  One request of
-// 1000 tokens, 64 rows on 8 K/V heads: 22.4 us with 4, 24.1 with 2, 23.7 with 8; 4 of 2000, 256 rows: 46.6, 46.4, 48.4.
+// Tiles of a range at least: fewer cost more in beginnings and partial results than they gain in workgroups, but for one or two
+// short requests.  us with 4 / 2: 8 requests of 200 tokens, 80 rows on 8 K/V heads 19.9 / 27.1; 4 of 500, 128 rows 30.6 / 32.8; 2 of
+// 1000, 128 rows 29.3 / 31.9; 40 heads of 33 rows, 300 tokens 15.4 / 17.2; one of 1000, 64 rows 21.9 / 20.8 (24.5 with 8); one of 300,
+// 128 rows 25.9 / 21.7.  4 of 2000, 256 rows: 45.3 with 2, 4 or 8.
 constexpr int kLeastRange = 4;
 constexpr int64_t kMostGroups = (int64_t(1) << 23);  // a launch holds fewer than 2^32 threads
 
 // Workgroups of a compute unit that the registers leave room for: the shared form, and the other one (`codes`: 8 bits, `tree`: nodes).
-// (Three of the shared form's smaller one at dh = 128 spill: 33 rows 44 us for 37.)
+// (Three of the shared form's smaller one at dh = 128 spill: 33 rows of 40 heads 41 us for 38.)
 HK_HOST_DEVICE constexpr int resident(int head_dim, int tiles) { return head_dim == 64 && tiles == 1 ? 3 : 2; }
 HK_HOST_DEVICE constexpr int resident_pieces(int head_dim, int tiles, bool codes, bool tree)
 {
@@ -57,13 +59,13 @@ constexpr int64_t kWholeBytes = 1 << 20, kMostSearched = 512;
 // tokens on 8 K/V heads, int8 23 / 27; 25 x 12 heads, 12 nodes, 16 bits 11 / 17.  Beyond 512 requests every workgroup's search for
 // its piece costs more than that: 1024 of 250 to 500 140 / 200, one of 32768 among them 368 / 241; so these are left alone.
 // Where it is ruled out:
-//   * Short requests are left whole, 512 tokens on average.  8 requests of 300 tokens and 8 K/V heads, int8: 6.7 us whole, 10.2
-//     cut; one request of 3000: 15.5 and 10.5.
+//   * Short requests are left whole, 512 tokens on average.  8 requests of 300 tokens and 8 K/V heads, int8: 6.9 us whole, 11.0
+//     cut; 16 bits, 560 tokens 13.3 and 13.5, 1125 tokens 18.8 and 17.7; one request of 3000, int8: 24.9 and 11.0.
 //   * Where they fill the chip, `want` workgroups.
 //   * Where they give every compute unit one: what the cut gains in balance, its merge and its shorter pieces lose.  8 requests x
-//     32 K/V heads, 560 / 1125 / 2250 / 6000 tokens on average (from half of the longest on), e4m3, one token: 11 / 19 / 35 / 86 us
-//     whole, 16 / 24 / 39 / 92 cut; 24 nodes over int8: 20 / 32 / 50 / 108 and 33 / 45 / 64 / 131.  dh = 64 (25 requests x 12 heads, 12
-//     nodes, 16 bits): 16 / 28 / 51 / 120 and 22 / 31 / 46 / 101.
+//     32 K/V heads, 560 / 1125 / 2250 / 6000 tokens on average (from half of the longest on), e4m3, one token: 12 / 20 / 33 / 82 us
+//     whole, 17 / 25 / 36 / 87 cut; 24 nodes over int8: 21 / 32 / 50 / 103 and 25 / 45 / 65 / 129.  dh = 64 (25 requests x 12 heads, 12
+//     nodes, 16 bits): 15 / 27 and 21 / 30, beyond that the cut is as fast or faster.
 inline bool left_whole(int64_t B, int64_t Hkv, int head_dim, bool codes, int64_t total_tokens, int64_t room, int64_t want)
 {
     const int64_t longest = room < total_tokens ? room : total_tokens, shares = B * Hkv < want ? B : (want + Hkv - 1) / Hkv;
@@ -93,8 +95,8 @@ inline Plan plan(int64_t B, int64_t T, int64_t H, int64_t Hkv, int head_dim, boo
     p.shared = all > kMaxTiles;
     p.extra = 0;
     if (p.shared) {
-        // two tiles a wavefront where one leaves rows for another workgroup: 16 requests of up to 8192 tokens, 512 rows 353 us
-        // for 479, 16 of 2000, 256 rows 78 for 93 (small batches lose: 4 of 2000 45 for 41)
+        // two tiles a wavefront where one leaves rows for another workgroup: 16 requests of up to 8192 tokens, 512 rows 354 us
+        // for 488, 16 of 2000, 256 rows 75 for 84 (small batches lose: 4 of 2000 45 for 43, one of 4000 47 for 44)
         p.tiles = all > kWaves ? 2 : 1;
         const int64_t held = 16 * kWaves * p.tiles;
         // tiles of the line at most: those of the tokens, a last one of each request that is not full, two of nodes
